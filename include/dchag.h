@@ -311,6 +311,95 @@ size_t dchag_workspace_bytes(dchag_dtype dt, int B, int C, int H, int W, int p, 
                              int n_levels, const int32_t *group_sizes, int which);
 
 /*
+ * Attention over packed sequences of tokens: what the spatial transformer behind the aggregation does with the
+ * [B,N,D] representation (paper Section 2.1: the aggregated token of every patch goes to the ViT), and its relative of
+ * autoregressive rollouts.  The rows of q, k and v are tokens of `sequences` sequences lying one behind the other: sequence s has
+ * the query rows q_starts[s] .. q_starts[s+1] and the key rows k_starts[s] .. k_starts[s+1], of which the first
+ * k_used[s] count if k_used is given (a cache with room to grow).  With Lq queries and Lk keys, the queries are the
+ * last Lq positions: key j lies r = j - (i + Lk - Lq) behind query i.  For head a and its key head a / (heads / kv_heads)
+ *
+ *   s_ij = scale <q_i, k_j> + bias[a][bucket(r)]          causal: only keys with r <= 0 are visible
+ *   out_i = sum_j P_ij v_j,   P_ij = exp(s_ij - lse_i),   lse_i = log sum_j exp(s_ij)
+ *
+ *   q, out [rows_q][heads][head_dim]     k, v [rows_k][kv_heads][head_dim]     lse [heads][rows_q] float
+ *
+ * A row that sees no key (Lk = 0, or causal and i + Lk - Lq < 0) has out = 0, lse = -inf, and no gradient.  Rows of
+ * q and out (of k and v) that belong to no sequence are neither read nor written.  What a pair that is not visible holds
+ * does not matter, nor do key rows that do not count: not even where they are not finite.
+ *
+ * The bias is learned per head and bucket of relative positions: bucket(r) = the number of borders <= |r|, plus
+ * n_borders + 1 if r > 0 and the call is not causal.  So bias is [heads][buckets] with buckets = n_borders + 1 (causal) or
+ * 2 (n_borders + 1).  An entry at or below -1e30 masks its pairs.
+ */
+typedef struct {
+  int32_t heads, kv_heads;          /* kv_heads divides heads                                            */
+  int32_t head_dim;                 /* 8, 16, ..., 128                                                   */
+  int32_t causal;                   /* 0 or 1                                                            */
+  int32_t sequences, rows_q, rows_k;/* >= 0                                                              */
+  float scale;                      /* > 0, or 0 for 1 / sqrt(head_dim)                                  */
+  int64_t ld_q, ld_k, ld_v, ld_out; /* elements from one row to the next: a multiple of 8, at least the  */
+  int64_t ld_dout, ld_dq, ld_dk, ld_dv; /* heads' columns, at most 2^23; 0 for rows without a gap.  The heads of a row
+                                       lie one behind the other (q, k and v may be columns of one tensor) */
+  const int32_t *q_starts, *k_starts;/* DEVICE, [sequences + 1], not decreasing.  Values outside 0 .. rows are taken as the
+                                       nearest inside: a call never leaves its tensors                   */
+  const int32_t *k_used;            /* DEVICE, [sequences], or NULL: all key rows count                  */
+  const void *bias;                 /* [heads][buckets], type dt, or NULL: no bias                       */
+  const int32_t *borders;           /* HOST, [n_borders], with a bias: increasing, from >= 1 to <= 1024  */
+  int32_t n_borders;                /* with a bias: 1 .. 63                                              */
+} dchag_attention;
+
+/*
+ * Forward pass.  workspace: dchag_attend_workspace_bytes(dt, att, 0) bytes, 256-byte aligned.
+ * Results do not depend on what other sequences a call holds, nor on how often it runs, up to the choice of kernel, which
+ * goes by rows_q, rows_k, sequences and the head counts.
+ * Errors: NULL att, starts, or a tensor that has rows; heads % kv_heads; head_dim; row strides; borders (DCHAG_ERR_SHAPE).
+ */
+int dchag_attend(dchag_dtype dt, const dchag_attention *att, const void *q, const void *k, const void *v,
+                 void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Backward pass: gradients of a loss with dL/d(out) = dout.  out and lse are those of the forward call.
+ *   dq, dk, dv   shaped like q, k, v        dbias [heads][buckets] or NULL (not wanted)
+ * Gradients are overwritten, not accumulated into; gradients of shared key heads are sums over their group.  No sum uses
+ * atomics: results are reproducible run to run.  workspace: dchag_attend_workspace_bytes(dt, att, 1) bytes.
+ * Errors: as dchag_attend; DCHAG_ERR_SHAPE for dbias without a bias.
+ */
+int dchag_attend_backward(dchag_dtype dt, const dchag_attention *att, const void *q, const void *k, const void *v,
+                          const void *out, const float *lse, const void *dout, void *dq, void *dk, void *dv, void *dbias,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace in bytes of a call on the current device (see dchag_workspace_bytes); which = 0: forward, 1: backward; 0 on invalid arguments. */
+size_t dchag_attend_workspace_bytes(dchag_dtype dt, const dchag_attention *att, int which);
+
+/*
+ * Activations kept in 8 bits between the two passes: what dchag_forward_keep does for the aggregation at full width, for the
+ * tensors around it (the tokens, or the input of a linear layer) at half of bf16's and a quarter of fp32's.  A row of D values
+ * becomes D codes (OCP e4m3) and one exponent byte for every 32 of them (the last block may be shorter):
+ *
+ *   value = code * 2^(byte - 127),   byte = the smallest >= 0 with  max |finite value of the block| <= 448 * 2^(byte - 127)
+ *
+ * so that scaling is exact, nothing saturates, and the one rounding (to nearest, ties to even) is off by at most 2^-4 of a value, or
+ * 2^-10 * 2^(byte - 127) where that is more.  (A value beyond 1.875 * 2^127 becomes that.)  A value that is not finite is kept as NaN.
+ *   x [rows][D] with ld elements from row to row (0: D)      codes [rows][D]      scales [rows][(D + 31) / 32]
+ * Errors: NULL pointers; D % 8 != 0, D < 8, D > 2^20; ld < D, ld % 8 != 0 or ld > 2^23; rows < 0.
+ */
+int dchag_pack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void *x, void *codes, void *scales, void *stream);
+int dchag_unpack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void *codes, const void *scales, void *x, void *stream);
+
+/*
+ * Weight and bias gradient of a linear layer y = x W^T + b whose input was kept in 8 bits, straight from the codes:
+ *
+ *   dW[o][i] = sum over rows of dy[row][o] x8[row][i]      db[o] = sum over rows of dy[row][o]   (db may be NULL)
+ *
+ *   dy [rows][d_out] with ld elements from row to row (0: d_out)    codes, scales of dchag_pack8 with D = d_in    dW [d_out][d_in]
+ * workspace: dchag_weight_grad8_workspace_bytes(...) bytes.  Sums are fp32 in a fixed order.
+ * Errors: NULL pointers; d_out, d_in % 8 != 0 or < 8; ld as above; rows < 0.  rows = 0 gives zeros.
+ */
+int dchag_weight_grad8(dchag_dtype dt, int rows, int d_out, int d_in, int64_t ld, const void *dy, const void *codes,
+                       const void *scales, void *dW, void *db, void *workspace, size_t workspace_bytes, void *stream);
+size_t dchag_weight_grad8_workspace_bytes(dchag_dtype dt, int rows, int d_out, int d_in);
+
+/*
  * Stage timing, a diagnostic for benchmarks (not part of the paper's method).  Between
  * dchag_profile_begin and dchag_profile_end every kernel the library launches is bracketed
  * by a pair of HIP events recorded on the call's own stream; dchag_profile_end waits for the
@@ -345,9 +434,17 @@ typedef enum {
   DCHAG_STAGE_BWD_CHANNEL_MIX = 18,/* backward of a linear level                                */
   DCHAG_STAGE_FOLD_VALUE = 19,     /* value projection folded into the tokenizer (weight-only)  */
   DCHAG_STAGE_TOKENIZE_ATTEND = 20,/* tokenizer fused with an attention first level             */
-  DCHAG_STAGE_KEY_PREP = 21        /* projected queries and query-folded keys of one level (level
+  DCHAG_STAGE_KEY_PREP = 21,       /* projected queries and query-folded keys of one level (level
                                       >= 1) or of all levels of the call at once (level 0); the
                                       bf16 path's form of stages 1 and 2 (weight-only)            */
+  DCHAG_STAGE_ATTEND = 22,         /* attention over packed sequences                          */
+  DCHAG_STAGE_ATTEND_JOIN = 23,    /* its partial results over stretches of the keys joined    */
+  DCHAG_STAGE_BWD_ATTEND_QUERY = 24,/* its gradients at the queries (and the bias, per tile)   */
+  DCHAG_STAGE_BWD_ATTEND_KEY = 25, /* its gradients at the keys and values                     */
+  DCHAG_STAGE_BWD_ATTEND_BIAS = 26,/* the bias gradient's parts summed                         */
+  DCHAG_STAGE_PACK8 = 27,          /* activations to 8 bits                                    */
+  DCHAG_STAGE_UNPACK8 = 28,        /* and back                                                 */
+  DCHAG_STAGE_WEIGHT_GRAD8 = 29    /* weight gradient of a linear layer with an 8-bit input    */
 } dchag_stage;
 
 typedef struct {

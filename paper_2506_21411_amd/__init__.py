@@ -8,8 +8,8 @@ PyTorch fallback: if the library is missing, importing `binding` functions raise
 from .binding import (  # noqa: F401
     DCHAG_BF16, DCHAG_F32, STATIC_SCRATCH_BYTES, DchagError, LevelGrads, LevelWeights, dchag_aggregate_level,
     dchag_aggregate_level_static,
-    dchag_backward, dchag_debug_reload, dchag_fold_value, dchag_forward,
-    dchag_forward_folded, dchag_forward_keep, dchag_forward_pos, dchag_forward_prefolded, dchag_profile_begin,
-    dchag_profile_end, dchag_tokenize, dchag_workspace_bytes, dchag_yardstick_copy, dchag_yardstick_mfma, dchag_yardstick_read, library_path,
-    load_library, use_library,
+    dchag_attend, dchag_attend_backward, dchag_backward, dchag_debug_reload, dchag_fold_value, dchag_forward,
+    dchag_forward_folded, dchag_forward_keep, dchag_forward_pos, dchag_forward_prefolded, dchag_pack8, dchag_profile_begin,
+    dchag_profile_end, dchag_tokenize, dchag_unpack8, dchag_weight_grad8, dchag_workspace_bytes, dchag_yardstick_copy, dchag_yardstick_mfma, dchag_yardstick_read, library_path,
+    load_library, log_borders, use_library,
 )

@@ -40,6 +40,14 @@ class _CLevelGrads(ctypes.Structure):
                 ("dbq", ctypes.c_void_p), ("dbk", ctypes.c_void_p), ("dbv", ctypes.c_void_p), ("dbo", ctypes.c_void_p)]
 
 
+class _CAttention(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("heads", "kv_heads", "head_dim", "causal", "sequences", "rows_q", "rows_k")]
+                + [("scale", ctypes.c_float)]
+                + [(n, ctypes.c_int64) for n in ("ld_q", "ld_k", "ld_v", "ld_out", "ld_dout", "ld_dq", "ld_dk", "ld_dv")]
+                + [(n, ctypes.c_void_p) for n in ("q_starts", "k_starts", "k_used", "bias", "borders")]
+                + [("n_borders", ctypes.c_int32)])
+
+
 class _CStageTime(ctypes.Structure):
     _fields_ = [("stage", ctypes.c_int32), ("level", ctypes.c_int32), ("ms", ctypes.c_float)]
 
@@ -47,7 +55,9 @@ class _CStageTime(ctypes.Structure):
 STAGE_NAMES = {0: "tokenize", 1: "query", 2: "fold", 3: "scores", 4: "vproj", 5: "softmax_agg", 6: "oproj",
                7: "fused_vagg", 8: "channel_mix", 9: "tokenize_mix", 10: "head_sums", 11: "head_vproj",
                12: "bwd_oproj", 13: "bwd_value", 14: "bwd_softmax", 15: "bwd_tokens", 16: "bwd_key_query",
-               17: "bwd_tokenize", 18: "bwd_channel_mix", 19: "fold_value", 20: "tokenize_attend", 21: "key_prep"}
+               17: "bwd_tokenize", 18: "bwd_channel_mix", 19: "fold_value", 20: "tokenize_attend", 21: "key_prep",
+               22: "attend", 23: "attend_join", 24: "bwd_attend_query", 25: "bwd_attend_key", 26: "bwd_attend_bias", 27: "pack8",
+               28: "unpack8", 29: "weight_grad8"}
 
 LEVEL_ATTENTION, LEVEL_LINEAR = 0, 1
 
@@ -144,6 +154,21 @@ def load_library():
     lib.dchag_backward_kept.argtypes = lib.dchag_backward.argtypes
     lib.dchag_workspace_bytes.restype = sz
     lib.dchag_workspace_bytes.argtypes = [i] * 9 + [ctypes.POINTER(ctypes.c_int32), i]
+    att, i64 = ctypes.POINTER(_CAttention), ctypes.c_int64
+    lib.dchag_attend.restype = i
+    lib.dchag_attend.argtypes = [i, att] + [vp] * 6 + [sz, vp]
+    lib.dchag_attend_backward.restype = i
+    lib.dchag_attend_backward.argtypes = [i, att] + [vp] * 11 + [sz, vp]
+    lib.dchag_attend_workspace_bytes.restype = sz
+    lib.dchag_attend_workspace_bytes.argtypes = [i, att, i]
+    lib.dchag_pack8.restype = i
+    lib.dchag_pack8.argtypes = [i, i64, i, i64] + [vp] * 4
+    lib.dchag_unpack8.restype = i
+    lib.dchag_unpack8.argtypes = [i, i64, i, i64] + [vp] * 4
+    lib.dchag_weight_grad8.restype = i
+    lib.dchag_weight_grad8.argtypes = [i, i, i, i, i64] + [vp] * 6 + [sz, vp]
+    lib.dchag_weight_grad8_workspace_bytes.restype = sz
+    lib.dchag_weight_grad8_workspace_bytes.argtypes = [i, i, i, i]
     lib.dchag_strerror.restype = ctypes.c_char_p
     lib.dchag_strerror.argtypes = [i]
     lib.dchag_version.restype = ctypes.c_char_p
@@ -416,6 +441,192 @@ def dchag_backward(x: torch.Tensor, We: torch.Tensor, be: Optional[torch.Tensor]
     _check(fn(dt, B, C, H, W, p, D, heads, _ptr(x), _ptr(We, x), _ptr(be, x), _ptr(ce, x),
               len(levels), arr, _ptr(dout, x), _ptr(dx, x), _ptr(dWe, x), _ptr(dtok_bias, x), garr,
               ctypes.c_void_p(workspace.data_ptr()), workspace.numel(), _stream(stream)))
+
+
+def log_borders(buckets: int, max_distance: int) -> List[int]:
+    """Borders for `buckets` buckets a side: the first half of the distances have a bucket each, the other buckets widen by a constant
+    factor up to max_distance, from which on all distances share the last.  Border b of the second half is the smallest whole distance r with
+    r >= e (max_distance / e)^((b - e) / (buckets - e)), e = buckets // 2, found in whole numbers."""
+    e = buckets // 2
+    if buckets < 2 or max_distance <= e:
+        raise ValueError("need at least two buckets, and a max_distance beyond the first half of them")
+    n, out = buckets - e, list(range(1, e + 1))
+    for k in range(1, n):
+        r, want = out[-1] + 1, e ** (n - k) * max_distance ** k
+        while r ** n < want:
+            r += 1
+        out.append(r)
+    return out
+
+
+def _rows_of(t: torch.Tensor, name: str, heads: Optional[int] = None, d: Optional[int] = None) -> int:
+    """Elements from one row to the next of [rows, heads, d] whose heads lie one behind the other."""
+    if t.dim() != 3 or (heads is not None and (t.shape[1], t.shape[2]) != (heads, d)):
+        raise ValueError(f"{name} must be [rows, heads, head_dim]" + (f" with {heads} heads of {d}" if heads is not None else ""))
+    if t.numel() and ((t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+        raise ValueError(f"the heads of a row of {name} must lie one behind the other")
+    return int(t.stride(0)) if t.shape[0] > 1 else 0
+
+
+def _dev_ptr(t: Optional[torch.Tensor], like: Optional[torch.Tensor], name: str, dtype: Optional[torch.dtype] = None):
+    """Address of a tensor on the current device, of the given dtype or like's; its strides are the caller's business."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a tensor on the current device")
+    if t.dtype != (like.dtype if dtype is None else dtype):
+        raise TypeError(f"{name} must be {like.dtype if dtype is None else dtype}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders):
+    """The C struct of a call, and what it points to on the host."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k and v must be [rows, heads, head_dim]")
+    heads, d, kv_heads = q.shape[1], q.shape[2], k.shape[1]
+    a = _CAttention()
+    a.heads, a.kv_heads, a.head_dim, a.causal = heads, kv_heads, d, int(bool(causal))
+    a.rows_q, a.rows_k, a.scale = q.shape[0], k.shape[0], float(scale)
+    if v.shape != k.shape:
+        raise ValueError("k and v must have the same shape")
+    a.ld_q, a.ld_k, a.ld_v = _rows_of(q, "q"), _rows_of(k, "k", kv_heads, d), _rows_of(v, "v", kv_heads, d)
+    for name, t, n in (("q_starts", q_starts, None), ("k_starts", k_starts, 0), ("k_used", k_used, -1)):
+        if t is None:
+            continue
+        if t.dim() != 1 or not t.is_contiguous() or t.numel() < 1 - (n == -1):
+            raise ValueError(f"{name} must be a contiguous vector")
+        if n is not None and t.numel() != q_starts.numel() + n:
+            raise ValueError(f"{name} does not have as many sequences as q_starts")
+    a.sequences = q_starts.numel() - 1
+    a.q_starts = _dev_ptr(q_starts, None, "q_starts", torch.int32)
+    a.k_starts = _dev_ptr(k_starts, None, "k_starts", torch.int32)
+    a.k_used = _dev_ptr(k_used, None, "k_used", torch.int32)
+    host = None
+    if (bias is None) != (borders is None):
+        raise ValueError("bias and borders come together")
+    if bias is not None:
+        host = (ctypes.c_int32 * max(1, len(borders)))(*[int(b) for b in borders])
+        if tuple(bias.shape) != (heads, (len(borders) + 1) * (1 if causal else 2)) or not bias.is_contiguous():
+            raise ValueError("bias must be contiguous, [heads, buckets] with one bucket more than borders, twice as many if not causal")
+        a.bias, a.n_borders = _dev_ptr(bias, q, "bias"), len(borders)
+        a.borders = ctypes.cast(host, ctypes.c_void_p)
+    return a, host
+
+
+def dchag_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: torch.Tensor, k_starts: torch.Tensor, *,
+                 causal: bool = False, scale: float = 0.0, k_used: Optional[torch.Tensor] = None,
+                 bias: Optional[torch.Tensor] = None, borders: Optional[Sequence[int]] = None,
+                 out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None, stream=None):
+    """(out [rows_q, heads, d], lse [heads, rows_q] float32) of attention over packed sequences: q [rows_q, heads, d], k and v
+    [rows_k, kv_heads, d], int32 starts [sequences + 1] on the device.  Rows of a tensor may have gaps between them (columns of a
+    joint projection).  Rows of no sequence are not written: give an `out` of your own if they are read later."""
+    a, host = _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders)
+    dt, lib = _dt(q), load_library()
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    a.ld_out = _rows_of(out, "out", q.shape[1], q.shape[2])
+    if lse is None:
+        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+    if out.shape != q.shape or tuple(lse.shape) != (q.shape[1], q.shape[0]) or not lse.is_contiguous():
+        raise ValueError("out must be shaped like q, lse [heads, rows_q] and contiguous")
+    if workspace is None:
+        workspace = _workspace(lib.dchag_attend_workspace_bytes(dt, ctypes.byref(a), 0), q.device)
+    _check(lib.dchag_attend(dt, ctypes.byref(a), _dev_ptr(q, q, "q"), _dev_ptr(k, q, "k"), _dev_ptr(v, q, "v"),
+                            _dev_ptr(out, q, "out"), _dev_ptr(lse, None, "lse", torch.float32),
+                            ctypes.c_void_p(workspace.data_ptr()), workspace.numel(), _stream(stream)))
+    return out, lse
+
+
+def dchag_attend_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                          dout: torch.Tensor, q_starts: torch.Tensor, k_starts: torch.Tensor, *, causal: bool = False,
+                          scale: float = 0.0, k_used: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                          borders: Optional[Sequence[int]] = None, dq: Optional[torch.Tensor] = None,
+                          dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
+                          dbias: Optional[torch.Tensor] = None, want_dbias: bool = True,
+                          workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dq, dk, dv, dbias or None) of <dout, dchag_attend(...)>; out and lse are those of the forward call with the same arguments.
+    Rows of no sequence are not written."""
+    a, host = _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders)
+    dt, lib = _dt(q), load_library()
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
+    if bias is None and dbias is not None:
+        raise ValueError("dbias without a bias")
+    if bias is not None and want_dbias and dbias is None:
+        dbias = torch.empty_like(bias)
+    if dbias is not None and (dbias.shape != bias.shape or not dbias.is_contiguous()):
+        raise ValueError("dbias must be shaped like bias and contiguous")
+    for name, t, like in (("out", out, q), ("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+        if t.shape != like.shape:
+            raise ValueError(f"{name} must be shaped like {'q' if like is q else 'k and v'}")
+        setattr(a, "ld_" + name, _rows_of(t, name))
+    if tuple(lse.shape) != (q.shape[1], q.shape[0]) or not lse.is_contiguous():
+        raise ValueError("lse must be [heads, rows_q] and contiguous")
+    if workspace is None:
+        workspace = _workspace(lib.dchag_attend_workspace_bytes(dt, ctypes.byref(a), 1), q.device)
+    ptrs = [_dev_ptr(t, q, n) for n, t in (("q", q), ("k", k), ("v", v), ("out", out))]
+    ptrs += [_dev_ptr(lse, None, "lse", torch.float32)]
+    ptrs += [_dev_ptr(t, q, n) for n, t in (("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv), ("dbias", dbias))]
+    _check(lib.dchag_attend_backward(dt, ctypes.byref(a), *ptrs, ctypes.c_void_p(workspace.data_ptr()), workspace.numel(),
+                                     _stream(stream)))
+    return dq, dk, dv, dbias
+
+
+def _matrix(t: torch.Tensor, name: str) -> int:
+    """Elements from one row to the next of a matrix whose rows have no gaps inside."""
+    if t.dim() != 2 or (t.numel() and t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a matrix with adjacent columns")
+    return int(t.stride(0)) if t.shape[0] > 1 else 0
+
+
+def _codes8(codes: torch.Tensor, scales: torch.Tensor, rows: int, D: int) -> None:
+    if tuple(codes.shape) != (rows, D) or tuple(scales.shape) != (rows, (D + 31) // 32) or not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError("codes must be [rows, D] and scales [rows, (D + 31) // 32], contiguous")
+
+
+def dchag_pack8(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
+    """(codes uint8 [rows, D], scales uint8 [rows, (D + 31) // 32]): the rows of x in 8 bits, one exponent for every 32 values."""
+    ld, (rows, D) = _matrix(x, "x"), x.shape
+    codes = torch.empty((rows, D), dtype=torch.uint8, device=x.device) if codes is None else codes
+    scales = torch.empty((rows, (D + 31) // 32), dtype=torch.uint8, device=x.device) if scales is None else scales
+    _codes8(codes, scales, rows, D)
+    _check(load_library().dchag_pack8(_dt(x), rows, D, ld, _dev_ptr(x, x, "x"), _dev_ptr(codes, None, "codes", torch.uint8),
+                                      _dev_ptr(scales, None, "scales", torch.uint8), _stream(stream)))
+    return codes, scales
+
+
+def dchag_unpack8(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
+                  out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The rows that codes and scales (dchag_pack8) stand for."""
+    rows, D = codes.shape
+    _codes8(codes, scales, rows, D)
+    out = torch.empty((rows, D), dtype=dtype, device=codes.device) if out is None else out
+    if tuple(out.shape) != (rows, D):
+        raise ValueError("out must be [rows, D]")
+    _check(load_library().dchag_unpack8(_dt(out), rows, D, _matrix(out, "out"), _dev_ptr(codes, None, "codes", torch.uint8),
+                                        _dev_ptr(scales, None, "scales", torch.uint8), _dev_ptr(out, out, "out"), _stream(stream)))
+    return out
+
+
+def dchag_weight_grad8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, dW: Optional[torch.Tensor] = None,
+                       db: Optional[torch.Tensor] = None, want_db: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dW [d_out, d_in], db [d_out] or None) of a linear layer: dy [rows, d_out], its input in 8 bits (dchag_pack8)."""
+    ld, (rows, d_out), d_in = _matrix(dy, "dy"), dy.shape, codes.shape[-1]
+    _codes8(codes, scales, rows, d_in)
+    dW = torch.empty((d_out, d_in), dtype=dy.dtype, device=dy.device) if dW is None else dW
+    db = torch.empty((d_out,), dtype=dy.dtype, device=dy.device) if db is None and want_db else db
+    if tuple(dW.shape) != (d_out, d_in) or (db is not None and tuple(db.shape) != (d_out,)):
+        raise ValueError("dW must be [d_out, d_in], db [d_out]")
+    dt, lib = _dt(dy), load_library()
+    if workspace is None:
+        workspace = _workspace(lib.dchag_weight_grad8_workspace_bytes(dt, rows, d_out, d_in), dy.device)
+    _dev_ptr(dW, dy, "dW"), _dev_ptr(db, dy, "db")
+    _check(lib.dchag_weight_grad8(dt, rows, d_out, d_in, ld, _dev_ptr(dy, dy, "dy"), _dev_ptr(codes, None, "codes", torch.uint8),
+                                  _dev_ptr(scales, None, "scales", torch.uint8), _ptr(dW, dy), _ptr(db, dy),
+                                  ctypes.c_void_p(workspace.data_ptr()), workspace.numel(), _stream(stream)))
+    return dW, db
 
 
 def dchag_yardstick_mfma(iters: int, sink: torch.Tensor, stream=None) -> float:

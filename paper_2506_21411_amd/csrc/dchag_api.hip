@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "dchag_dev.h"
+#include "host_base.h"
 #include "k_generic.h"
 #include "k_mfma.h"
 #include "k_fused.h"
@@ -117,10 +118,6 @@ SwitchTable g_switches;
 // The value of a switch, or nullptr when it is not set.
 inline const char* dbg(Switch s) { return g_switches.set[s] ? g_switches.value[s] : nullptr; }
 
-constexpr size_t kAlign = 256;
-inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
-inline size_t elem_size(dchag_dtype dt) { return dt == DCHAG_F32 ? 4 : 2; }
-inline bool misaligned(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u); }
 inline int groups_of(int c_in, int g) { return (c_in + g - 1) / g; }
 
 // The bf16 MFMA path of a level needs 256-wide column slices that hold whole heads or lie inside one.
@@ -140,7 +137,6 @@ struct LevelWs {
   int splits;                      // fast path: items a group's chunks are dealt to (vagg_splits)
 };
 
-int compute_units();
 
 // Items the value GEMM of a level deals a group's chunks of 8 channels to, so that a level of few groups (the flat
 // baseline, the top of a hierarchy) still fills the chip: 1, 2, 4 or 8, at most what leaves two items per compute unit and the chunks of
@@ -262,70 +258,6 @@ ForwardWs forward_ws(dchag_dtype dt, int B, int C, int N, int pp, int D, int hea
   }
   w.total = off;
   return w;
-}
-
-inline int launch_status() { return hipGetLastError() == hipSuccess ? DCHAG_OK : DCHAG_ERR_LAUNCH; }
-
-// Optional stage timing (dchag_profile_begin / dchag_profile_end): an event pair per launch.
-struct StageRecord {
-  hipEvent_t start, stop;
-  int stage, level;
-};
-bool g_profiling = false;
-int g_level = 0;
-std::vector<StageRecord> g_records;
-// The level a stage record is filed under; written only while a profile is being taken.
-inline void set_level(int level) {
-  if (g_profiling) g_level = level;
-}
-
-struct StageTimer {
-  hipStream_t st;
-  bool on;
-  StageRecord rec;
-  StageTimer(int stage, hipStream_t s) : st(s), on(g_profiling) {
-    if (!on) return;
-    rec.stage = stage;
-    rec.level = g_level;
-    if (hipEventCreate(&rec.start) != hipSuccess || hipEventCreate(&rec.stop) != hipSuccess) {
-      on = false;
-      return;
-    }
-    (void)hipEventRecord(rec.start, st);
-  }
-  ~StageTimer() {
-    if (!on) return;
-    (void)hipEventRecord(rec.stop, st);
-    g_records.push_back(rec);
-  }
-};
-
-// Compute units of the CURRENT device (looked up once per device; 256 without a device).
-constexpr int kMaxDevices = 64;
-int compute_units() {
-  static std::atomic<int> cus[kMaxDevices];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return 256;
-  int n = cus[dev].load(std::memory_order_relaxed);
-  if (n) return n;
-  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < kXcds) n = 256;
-  cus[dev].store(n, std::memory_order_relaxed);
-  return n;
-}
-
-// Raises a kernel's dynamic-LDS limit to at least `bytes`, once per (device, kernel): later launches only look the
-// table up.  Returns 0 or DCHAG_ERR_LAUNCH.
-int ensure_dynamic_lds(const void* kernel, int bytes) {
-  static std::mutex mu;
-  static std::unordered_map<const void*, int> done[kMaxDevices];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return DCHAG_ERR_LAUNCH;
-  std::lock_guard<std::mutex> lock(mu);
-  auto it = done[dev].find(kernel);
-  if (it != done[dev].end() && it->second >= bytes) return DCHAG_OK;
-  if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return DCHAG_ERR_LAUNCH;
-  done[dev][kernel] = bytes;
-  return DCHAG_OK;
 }
 
 bool force_generic() {

@@ -1,0 +1,1040 @@
+// Attention over packed sequences of tokens, with grouped heads, a causal mask and a learned relative position bias by buckets,
+// and its backward pass.  For head a of a sequence with Lq queries and Lk keys, r = j - (i + Lk - Lq) the position of key j
+// relative to query i (the queries are the sequence's last positions):
+//
+//   s_ij = scale <q_i, k_j> + bias[a][bucket(r)]     (causal: only r <= 0)
+//   o_i  = sum_j P_ij v_j,   P_ij = exp(s_ij - lse_i),   lse_i = log sum_j exp s_ij
+//   dP_ij = <do_i, v_j>,  dS_ij = P_ij (dP_ij - <do_i, o_i>),  dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,
+//   dv_j = sum_i P_ij do_i,  dbias[a][b] = sum over the pairs of bucket b of dS_ij
+//
+// Scores, softmax statistics and sums are fp32; for bf16 tensors P and dS are rounded to bf16 once, as operands of the matrix
+// instructions (their sums of products are fp32).  Exponentials are taken to base 2 of scores scaled by log2(e).
+//
+// Layout shared by all kernels here: products are formed so that the 16 columns of an accumulator block are the rows a wavefront
+// owns (queries, or keys in k_attend_dkv) and its 16 rows are those of the tile that lies in LDS: lane l holds, for its own row
+// l % 16, the tile rows 4 (l / 16) + 0..3.  A softmax row is then in-lane work plus two lane exchanges, rescaling is one factor
+// a lane, and two such blocks are, without any exchange, the operand of the next product over 32 tile rows in the order
+// {4 g + 0..3, 16 + 4 g + 0..3}, g = l / 16; the other operand is read from LDS in the same order (transposing reads).
+#pragma once
+#include "dchag_dev.h"
+
+namespace dchag {
+
+constexpr int kMaxBorders = 63;
+constexpr int kMaxDistance = 1024;     // of the last border: bounds the tables in LDS
+constexpr int kTileKeys = 64;          // rows of a tile in LDS
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -3.4028234663852886e38f;
+constexpr float kNegInf = -__builtin_inff();
+// A bias entry at or below this masks its pairs, like -inf (a mask written as a type's lowest value would not survive the scaling).
+constexpr float kMaskBias = -1e30f;
+// The running maximum is moved only when a tile's exceeds it by this much (base 2): what is added up stays below 2^8 of it.
+constexpr float kMaxSlack = 8.f;
+
+struct AttendArgs {
+  const int *q_starts, *k_starts, *k_used;
+  int sequences, rows_q, rows_k, heads, kv_heads, d, causal;
+  long ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;   // elements from one row to the next
+  float scale, c;                      // c = scale * log2(e)
+  const void* bias;                    // [heads][buckets] or NULL
+  int n_borders, last, side, buckets;  // last: the last border; side: buckets of one side
+  int borders[kMaxBorders];
+};
+
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+template <typename T> struct Frag;
+template <> struct Frag<bf16> { typedef bf16x8 type; };
+template <> struct Frag<float> { typedef f32x8 type; };
+
+// c += a x b over 32 contraction elements, eight of them a lane (8 g + 0..7 of it): one bf16 instruction, or eight fp32 ones,
+// each of which takes the same element of the four lanes g.
+__device__ __forceinline__ f32x4 mma(f32x4 c, bf16x8 a, bf16x8 b) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(f32x4 c, f32x8 a, f32x8 b) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+  return c;
+}
+
+static __device__ __align__(16) const unsigned char kZeros[16] = {0};
+
+// A tile of rows of DP elements in LDS, 16-byte chunks XOR-swizzled by the row so that both the 16 rows that a quarter-wavefront reads
+// at one chunk and the eight half-rows of 32 bytes that half a wavefront reads transposed lie in different banks.
+template <typename T, int DP>
+struct Tile {
+  static constexpr int kPitch = DP * (int)sizeof(T), kChunks = kPitch / 16, kElems = 16 / (int)sizeof(T);
+  static constexpr int kBytes = kTileKeys * kPitch;
+  static __device__ __forceinline__ int swz(int row) {
+    constexpr int per = kChunks >= 16 ? 1 : 16 / kChunks, wide = kChunks >= 16 ? 16 : kChunks;
+    return ((((row / per) & (wide / 2 - 1)) << 1) | ((row >> 3) & 1));
+  }
+  // Eight elements 32 ks + 8 g .. of row 16 blk + l % 16.
+  static __device__ __forceinline__ typename Frag<T>::type row_frag(const unsigned char* t, int blk, int ks, int lane) {
+    const int l16 = lane & 15, g = lane >> 4;
+    const unsigned char* p = t + (blk * 16 + l16) * kPitch;
+    if constexpr (sizeof(T) == 2) {
+      return *reinterpret_cast<const bf16x8*>(p + ((ks * 4 + g) ^ swz(l16)) * 16);
+    } else {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(p + ((ks * 8 + 2 * g) ^ swz(l16)) * 16);
+      const f32x4 b = *reinterpret_cast<const f32x4*>(p + ((ks * 8 + 2 * g + 1) ^ swz(l16)) * 16);
+      return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+  // Column 16 blk + l % 16 of the rows 32 s + {4 g + 0..3, 16 + 4 g + 0..3}.
+  static __device__ __forceinline__ typename Frag<T>::type col_frag(const unsigned char* t, int blk, int s, int lane) {
+    const int l16 = lane & 15, g = lane >> 4;
+    if constexpr (sizeof(T) == 2) {
+      typedef __attribute__((ext_vector_type(4))) short s16x4;
+      typedef __attribute__((address_space(3))) s16x4* tptr;
+      const int row = 4 * g + (l16 >> 2);
+      const unsigned char* p = t + row * kPitch + (((blk * 2 + ((l16 & 3) >> 1)) ^ swz(row)) * 16) + (l16 & 1) * 8 + s * 32 * kPitch;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr)p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tptr)(p + 16 * kPitch));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      f32x8 r;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int row = 4 * g + (j & 3) + (j >> 2) * 16;
+        r[j] = *reinterpret_cast<const float*>(t + (row + s * 32) * kPitch + (((blk * 4 + (l16 >> 2)) ^ swz(row)) * 16) + (l16 & 3) * 4);
+      }
+      return r;
+    }
+  }
+  // Element col of a row.
+  static __device__ __forceinline__ float at(const unsigned char* t, int row, int col) {
+    return to_f32(*reinterpret_cast<const T*>(t + row * kPitch + ((col / kElems) ^ swz(row)) * 16 + (col % kElems) * (int)sizeof(T)));
+  }
+  // Fills ROWS rows of a tile from rows base + row * ld (direct-to-LDS loads; NT threads take part, tid among them); rows from
+  // `rows` on and columns from d on come from zeros, so nothing outside the sequence and the head is read.
+  template <int ROWS, int NT>
+  static __device__ __forceinline__ void stage(const T* base, long ld, int rows, int d, unsigned char* lds, int tid) {
+    constexpr int kLoads = ROWS * kChunks / NT;
+    static_assert(kLoads * NT == ROWS * kChunks, "rows do not split over the threads");
+    if (rows >= ROWS && d == DP) {
+      const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(lptr_t)(lds + (tid & ~63) * 16));
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int idx = i * NT + tid, row = idx / kChunks, chunk = (idx % kChunks) ^ swz(row);
+        load16_to_lds_at(base, (unsigned)(row * (int)ld * (int)sizeof(T) + chunk * 16), lds0 + i * NT * 16);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int idx = i * NT + tid, row = idx / kChunks, chunk = (idx % kChunks) ^ swz(row);
+        const bool in = row < rows && chunk * kElems < d;
+        const void* src = in ? static_cast<const void*>(base + row * ld + chunk * kElems) : static_cast<const void*>(kZeros);
+        load16_to_lds(src, lds + (i * NT + (tid & ~63)) * 16);
+      }
+    }
+  }
+};
+
+// Eight elements 32 ks + 8 g .. of a row in global memory; zeros past the head's d.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type load_frag(const T* row, bool in, int ks, int g, int d) {
+  const int e = ks * 32 + g * 8;
+  typename Frag<T>::type r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = (T)0.f;
+  if (in && e < d) {
+    if constexpr (sizeof(T) == 2) {
+      r = *reinterpret_cast<const bf16x8*>(row + e);
+    } else {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(row + e), b = *reinterpret_cast<const f32x4*>(row + e + 4);
+      r = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+  return r;
+}
+// Four adjacent elements.
+__device__ __forceinline__ void store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
+__device__ __forceinline__ void store4(bf16* p, f32x4 v) { *reinterpret_cast<bf16x4*>(p) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]}; }
+
+// The values of lanes l and l ^ 32 (l ^ 16), the lower one first.
+struct LanePair {
+  float low, high;
+};
+template <class Two>
+__device__ __forceinline__ LanePair lane_pair(Two p) {
+  const unsigned low = p[0], high = p[1];                                    // a bit cast of a vector's element takes its first one
+  return {__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)};
+}
+__device__ __forceinline__ LanePair pair32(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  return lane_pair(__builtin_amdgcn_permlane32_swap(u, u, false, false));
+}
+__device__ __forceinline__ LanePair pair16(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  return lane_pair(__builtin_amdgcn_permlane16_swap(u, u, false, false));
+}
+// Maximum and sum over the four lanes of a row (lane, lane ^ 16, lane ^ 32, lane ^ 48); every one of them gets it.
+__device__ __forceinline__ float row_max(float v) {
+  LanePair p = pair32(v);
+  p = pair16(fmaxf(p.low, p.high));
+  return fmaxf(p.low, p.high);
+}
+__device__ __forceinline__ float row_sum(float v) {
+  LanePair p = pair32(v);
+  p = pair16(p.low + p.high);
+  return p.low + p.high;
+}
+
+// One sequence: rows q0 .. q0 + nq of the queries, k0 .. k0 + nk of the keys, and a tile of it.  The starts are data of the
+// device: whatever they hold, rows stay inside the tensors.
+struct Span {
+  int q0, nq, k0, nk, tile, tiles;
+};
+__device__ __forceinline__ void read_span(const AttendArgs& a, int s, int& q0, int& nq, int& k0, int& nk) {
+  q0 = min(max(a.q_starts[s], 0), a.rows_q);
+  nq = min(max(a.q_starts[s + 1], q0), a.rows_q) - q0;
+  k0 = min(max(a.k_starts[s], 0), a.rows_k);
+  nk = min(max(a.k_starts[s + 1], k0), a.rows_k) - k0;
+  if (a.k_used) nk = min(max(a.k_used[s], 0), nk);
+}
+// The sequence and tile that item idx is, the items of a sequence being count(nq, nk): 64 sequences at a time, one a lane.
+// False if there are not as many items.  Every wavefront finds it for itself.
+template <class Count>
+__device__ __forceinline__ bool find_span(const AttendArgs& a, int idx, Count count, Span& sp) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < a.sequences; s0 += 64) {
+    int q0 = 0, nq = 0, k0 = 0, nk = 0, n = 0;
+    if (s0 + lane < a.sequences) {
+      read_span(a, s0 + lane, q0, nq, k0, nk);
+      n = count(nq, nk);
+    }
+    int upto = n;
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) {
+      const int v = __shfl_up(upto, w);
+      if (lane >= w) upto += v;
+    }
+    const int total = __builtin_amdgcn_readlane(upto, 63);
+    if (idx < total) {
+      const int l = __builtin_ctzll(__ballot(idx < upto));
+      sp.q0 = __builtin_amdgcn_readlane(q0, l);
+      sp.nq = __builtin_amdgcn_readlane(nq, l);
+      sp.k0 = __builtin_amdgcn_readlane(k0, l);
+      sp.nk = __builtin_amdgcn_readlane(nk, l);
+      sp.tiles = __builtin_amdgcn_readlane(n, l);
+      sp.tile = idx - (__builtin_amdgcn_readlane(upto, l) - sp.tiles);
+      return true;
+    }
+    idx -= total;
+  }
+  return false;
+}
+
+// Which heads and which item a workgroup takes: key heads fastest, so that one XCD's workgroups (id % 8) share few of them.
+struct HeadItem {
+  int h, kvh, idx;
+};
+__device__ __forceinline__ HeadItem head_item(const AttendArgs& a, int id) {
+  const int group = a.heads / a.kv_heads, kvh = id % a.kv_heads, rest = id / a.kv_heads;
+  return {kvh * group + rest % group, kvh, rest / group};
+}
+
+// ---- the bias -------------------------------------------------------------------------------------------------------------
+// A pair whose distance is at least the last border has the last bucket of its side: a tile of such pairs only adds a constant.
+// The others look their value up by r in a table of the head in LDS that reaches kPad beyond the last border on both sides, as far
+// as a tile with one nearer pair can.
+constexpr int kPad = 128;
+__host__ __device__ inline int bias_table_size(int last) { return 2 * (last + kPad) + 1; }
+__device__ __forceinline__ int bucket_of(const AttendArgs& a, int r) {
+  const int dist = r < 0 ? -r : r;
+  int n = 0;
+  for (int b = 0; b < a.n_borders; ++b) n += dist >= a.borders[b];
+  return n + (r > 0 && !a.causal ? a.side : 0);
+}
+// An entry as it is added to scores to base 2.
+template <typename T>
+__device__ __forceinline__ float bias_value(const AttendArgs& a, int h, int bucket) {
+  const float v = to_f32(static_cast<const T*>(a.bias)[(size_t)h * a.buckets + bucket]);
+  return v <= kMaskBias ? kNegInf : v * kLog2e;
+}
+template <typename T, int NT>
+__device__ __forceinline__ void fill_bias_table(const AttendArgs& a, int h, float* table, int tid) {
+  const int n = bias_table_size(a.last), mid = a.last + kPad;
+  for (int i = tid; i < n; i += NT) table[i] = bias_value<T>(a, h, bucket_of(a, i - mid));
+}
+
+// Adds p v to acc pair by pair, leaving out the pairs with p = 0: what a masked pair's v holds then does not matter, not even a
+// NaN.  For tiles with masked pairs and with values that are not finite; acc and p as in the products over a tile of 64 rows.
+template <typename T, int DP, int NB, int MB>
+__device__ __forceinline__ void accumulate_pairs(f32x4 (&acc)[DP / 16][NB], const f32x4 (&p)[MB][NB], const unsigned char* t, int row0, int lane) {
+  const int l16 = lane & 15, g = lane >> 4;
+#pragma unroll 1
+  for (int j = 0; j < MB * 16; ++j) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float own = 0.f;
+#pragma unroll
+      for (int m = 0; m < MB * 4; ++m)
+        if (m == (j >> 4) * 4 + (j & 3)) own = p[m >> 2][nb][m & 3];
+      const float w = __shfl(own, l16 + 16 * ((j >> 2) & 3));
+#pragma unroll
+      for (int b = 0; b < DP / 16; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float v = Tile<T, DP>::at(t, row0 + j, b * 16 + 4 * g + r);
+          if (w != 0.f) acc[b][nb][r] += w * v;
+        }
+    }
+  }
+}
+// Whether a tile's rows row0 .. row0 + ROWS hold a value that is not finite (the same answer in every lane).
+template <typename T, int DP, int ROWS>
+__device__ __forceinline__ bool any_not_finite(const unsigned char* t, int row0, int lane) {
+  unsigned bad = 0;
+#pragma unroll
+  for (int i = 0; i < ROWS * Tile<T, DP>::kChunks / 64; ++i) {
+    const uint4 w = *reinterpret_cast<const uint4*>(t + row0 * Tile<T, DP>::kPitch + (i * 64 + lane) * 16);
+    const unsigned x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 2) bad |= ((x[k] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // exponent all ones carries into the sign
+      else bad |= ((x[k] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+    }
+  }
+  return __ballot(bad != 0) != 0;
+}
+
+// Workgroup: NW wavefronts of 16 NB queries of one head; the keys pass by in tiles of 64, two tiles of K and V in LDS, the next
+// one on its way (direct-to-LDS) while one is worked on.
+template <typename T, int DP, int NB, int NW, bool BIAS>
+__global__ __launch_bounds__(NW * 64, 2) void k_attend(AttendArgs a, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
+                                                       T* __restrict__ out, float* __restrict__ lse) {
+  typedef Tile<T, DP> TL;
+  typedef typename Frag<T>::type frag;
+  constexpr int KS = DP / 32, DB = DP / 16, MB = kTileKeys / 16, ROWS = NW * NB * 16, NT = NW * 64;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  float* table = reinterpret_cast<float*>(smem + 4 * TL::kBytes);
+  const HeadItem hi = head_item(a, blockIdx.x);
+  Span sp;
+  if (!find_span(a, hi.idx, [](int nq, int) { return (nq + ROWS - 1) / ROWS; }, sp)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
+  const int i0 = (a.causal ? sp.tiles - 1 - sp.tile : sp.tile) * ROWS;      // causal: the longest rows first
+  const int iw = i0 + wave * NB * 16, off = sp.nk - sp.nq;
+  const int kend = a.causal ? min(sp.nk, max(0, min(i0 + ROWS, sp.nq) + off)) : sp.nk;
+  const int tiles = (kend + kTileKeys - 1) / kTileKeys;
+  const T* kb_ = k + (long)sp.k0 * a.ld_k + hi.kvh * a.d;
+  const T* vb_ = v + (long)sp.k0 * a.ld_v + hi.kvh * a.d;
+  auto stage = [&](int t) {
+    unsigned char* to = smem + (t & 1) * 2 * TL::kBytes;
+    TL::template stage<kTileKeys, NT>(kb_ + (long)t * kTileKeys * a.ld_k, a.ld_k, sp.nk - t * kTileKeys, a.d, to, tid);
+    TL::template stage<kTileKeys, NT>(vb_ + (long)t * kTileKeys * a.ld_v, a.ld_v, sp.nk - t * kTileKeys, a.d, to + TL::kBytes, tid);
+  };
+  if (tiles > 0) stage(0);
+  float far_left = 0.f, far_right = 0.f;
+  if (BIAS) {
+    fill_bias_table<T, NT>(a, hi.h, table, tid);
+    far_left = bias_value<T>(a, hi.h, a.side - 1);
+    far_right = a.causal ? 0.f : bias_value<T>(a, hi.h, 2 * a.side - 1);
+  }
+  frag qf[NB][KS];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int i = iw + nb * 16 + l16;
+    const T* row = q + (long)(sp.q0 + min(i, sp.nq - 1)) * a.ld_q + hi.h * a.d;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[nb][ks] = load_frag<T>(row, i < sp.nq, ks, g, a.d);
+  }
+  f32x4 acc[DB][NB];
+  float m[NB], l[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    m[nb] = kLowest;
+    l[nb] = 0.f;
+#pragma unroll
+    for (int b = 0; b < DB; ++b) acc[b][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int lo = iw + off, top = lo + NB * 16 - 1;                          // positions of the wavefront's rows
+  for (int t = 0; t < tiles; ++t) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t + 1 < tiles) stage(t + 1);
+    const int kb = t * kTileKeys;
+    if (iw >= sp.nq || (a.causal && kb > top)) continue;
+    const unsigned char* K = smem + (t & 1) * 2 * TL::kBytes;
+    const unsigned char* V = K + TL::kBytes;
+    f32x4 s[MB][NB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) s[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const frag kf = TL::row_frag(K, mb, ks, lane);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) s[mb][nb] = mma(s[mb][nb], kf, qf[nb][ks]);
+      }
+    }
+    float mul = a.c, add = 0.f;
+    if (BIAS) {
+      const int rmax = kb + kTileKeys - 1 - lo, rmin = kb - top;
+      if (rmax <= -a.last) add = far_left;
+      else if (rmin >= a.last) add = far_right;
+      else {
+        mul = 1.f;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const float* tb = table + kb + 4 * g - (lo + nb * 16 + l16) + a.last + kPad;
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[mb][nb][r] = fmaf(s[mb][nb][r], a.c, tb[mb * 16 + r]);
+        }
+      }
+    }
+    const bool masked = kb + kTileKeys > sp.nk || (a.causal && kb + kTileKeys - 1 > lo);
+    if (masked) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const int end = a.causal ? min(sp.nk, lo + nb * 16 + l16 + 1) : sp.nk;   // keys before it are visible
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (kb + mb * 16 + 4 * g + r >= end) s[mb][nb][r] = kNegInf;
+      }
+    }
+    float mx[NB];
+    bool grow = false;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      mx[nb] = kNegInf;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) mx[nb] = fmaxf(mx[nb], fmaxf(fmaxf(s[mb][nb][0], s[mb][nb][1]), fmaxf(s[mb][nb][2], s[mb][nb][3])));
+      mx[nb] = fmaf(row_max(mx[nb]), mul, add);
+      grow |= mx[nb] > m[nb] + kMaxSlack;
+    }
+    if (__ballot(grow)) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const float next = fmaxf(m[nb], mx[nb]), f = __builtin_amdgcn_exp2f(m[nb] - next);
+        m[nb] = next;
+        l[nb] *= f;
+#pragma unroll
+        for (int b = 0; b < DB; ++b) acc[b][nb] *= f;
+      }
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float sub = add - m[nb];
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[mb][nb][r], mul, sub));
+          l[nb] += p;
+          s[mb][nb][r] = p;
+        }
+    }
+    if (masked && any_not_finite<T, DP, kTileKeys>(V, 0, lane)) {
+      accumulate_pairs<T, DP, NB, MB>(acc, s, V, 0, lane);
+      continue;
+    }
+#pragma unroll
+    for (int h2 = 0; h2 < MB / 2; ++h2) {
+      frag pf[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pf[nb][j] = (T)s[h2 * 2 + (j >> 2)][nb][j & 3];
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        const frag vf = TL::col_frag(V, b, h2, lane);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) acc[b][nb] = mma(acc[b][nb], vf, pf[nb]);
+      }
+    }
+  }
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int i = iw + nb * 16 + l16;
+    const float sum = row_sum(l[nb]), inv = sum == 0.f ? 0.f : 1.f / sum;     // sum 0: the row sees no key
+    if (i >= sp.nq) continue;
+    T* o = out + (long)(sp.q0 + i) * a.ld_o + hi.h * a.d;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+      if (b * 16 + 4 * g < a.d) store4(o + b * 16 + 4 * g, acc[b][nb] * inv);
+    if (g == 0) lse[(size_t)hi.h * a.rows_q + sp.q0 + i] = sum == 0.f ? kNegInf : (m[nb] + __builtin_amdgcn_logf(sum)) * kLn2;
+  }
+}
+
+// The same for few query rows a key head (single tokens against a cache): the rows of a workgroup are 16 of the pairs (query, head of
+// the group), so that a key head's rows are read once for its whole group, and the keys are dealt out: to `splits` workgroups in
+// stretches, inside one to its wavefronts tile by tile.  A wavefront streams its tiles of 32 keys through LDS of its own, without
+// a barrier; what the wavefronts have is joined in LDS, what the workgroups have by k_attend_join.  HBM-bound.
+constexpr int kFewRows = 16, kFewKeys = 32;
+template <typename T, int DP>
+constexpr int few_waves() { return DP * (int)sizeof(T) > 256 ? 2 : 4; }
+template <typename T, int DP>
+constexpr int few_lds() { return few_waves<T, DP>() * 4 * kFewKeys * DP * (int)sizeof(T); }
+
+template <typename T, int DP, bool BIAS>
+__global__ __launch_bounds__((few_waves<T, DP>() * 64)) void k_attend_few(AttendArgs a, int splits, const T* __restrict__ q, const T* __restrict__ k,
+                                                                        const T* __restrict__ v, T* __restrict__ out, float* __restrict__ lse,
+                                                                        float* __restrict__ part, float* __restrict__ part_ml) {
+  typedef Tile<T, DP> TL;
+  typedef typename Frag<T>::type frag;
+  constexpr int KS = DP / 32, DB = DP / 16, NW = few_waves<T, DP>(), kHalf = kFewKeys * TL::kPitch;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ float ml[NW][2][kFewRows];
+  const int group = a.heads / a.kv_heads, id = blockIdx.x;
+  const int kvh = id % a.kv_heads, split = id / a.kv_heads % splits, idx = id / a.kv_heads / splits;
+  Span sp;
+  if (!find_span(a, idx, [group](int nq, int) { return (nq * group + kFewRows - 1) / kFewRows; }, sp)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
+  const int rows = sp.nq * group, off = sp.nk - sp.nq;
+  const int row = min(sp.tile * kFewRows + l16, rows - 1);                   // past the end: the last one again, not written
+  const int i = row / group, h = kvh * group + row % group, pos = i + off;
+  const int first_pos = sp.tile * kFewRows / group + off, last_pos = min((sp.tile + 1) * kFewRows - 1, rows - 1) / group + off;
+  const int kend = a.causal ? min(sp.nk, max(0, last_pos + 1)) : sp.nk;
+  const int per = ((kend + splits - 1) / splits + kFewKeys - 1) / kFewKeys * kFewKeys;
+  const int c0 = min(split * per, kend), c1 = min(c0 + per, kend);
+  const int tiles = (c1 - c0 + kFewKeys - 1) / kFewKeys;
+  const T* kb_ = k + (long)sp.k0 * a.ld_k + kvh * a.d;
+  const T* vb_ = v + (long)sp.k0 * a.ld_v + kvh * a.d;
+  unsigned char* mine = smem + wave * 4 * kHalf;
+  auto stage = [&](int t, int slot) {
+    const int kb = c0 + t * kFewKeys;
+    TL::template stage<kFewKeys, 64>(kb_ + (long)kb * a.ld_k, a.ld_k, c1 - kb, a.d, mine + slot * 2 * kHalf, lane);
+    TL::template stage<kFewKeys, 64>(vb_ + (long)kb * a.ld_v, a.ld_v, c1 - kb, a.d, mine + slot * 2 * kHalf + kHalf, lane);
+  };
+  if (wave < tiles) stage(wave, 0);
+  frag qf[KS];
+  const T* qrow = q + (long)(sp.q0 + i) * a.ld_q + h * a.d;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) qf[ks] = load_frag<T>(qrow, true, ks, g, a.d);
+  float far_left = 0.f, far_right = 0.f;
+  if (BIAS) {
+    far_left = bias_value<T>(a, h, a.side - 1);
+    far_right = a.causal ? 0.f : bias_value<T>(a, h, 2 * a.side - 1);
+  }
+  f32x4 acc[DB][1];
+#pragma unroll
+  for (int b = 0; b < DB; ++b) acc[b][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = kLowest, l = 0.f;
+  for (int t = wave, slot = 0; t < tiles; t += NW, slot ^= 1) {
+    __builtin_amdgcn_s_waitcnt((0 << 8) | (7 << 4));                         // vmcnt(0) lgkmcnt(0): this tile is here, the one before is read
+    __builtin_amdgcn_sched_barrier(0);
+    if (t + NW < tiles) stage(t + NW, slot ^ 1);
+    const unsigned char* K = mine + slot * 2 * kHalf;
+    const unsigned char* V = K + kHalf;
+    const int kb = c0 + t * kFewKeys;
+    f32x4 s[2][1];
+#pragma unroll
+    for (int mb = 0; mb < 2; ++mb) {
+      s[mb][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) s[mb][0] = mma(s[mb][0], TL::row_frag(K, mb, ks, lane), qf[ks]);
+    }
+    float mul = a.c, add = 0.f;
+    if (BIAS) {
+      if (kb + kFewKeys - 1 - first_pos <= -a.last) add = far_left;
+      else if (kb - last_pos >= a.last) add = far_right;
+      else {
+        mul = 1.f;
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            s[mb][0][r] = fmaf(s[mb][0][r], a.c, bias_value<T>(a, h, bucket_of(a, kb + mb * 16 + 4 * g + r - pos)));
+      }
+    }
+    const bool masked = kb + kFewKeys > c1 || (a.causal && kb + kFewKeys - 1 > first_pos);
+    if (masked) {
+      const int end = a.causal ? min(c1, pos + 1) : c1;
+#pragma unroll
+      for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (kb + mb * 16 + 4 * g + r >= end) s[mb][0][r] = kNegInf;
+    }
+    float mx = kNegInf;
+#pragma unroll
+    for (int mb = 0; mb < 2; ++mb) mx = fmaxf(mx, fmaxf(fmaxf(s[mb][0][0], s[mb][0][1]), fmaxf(s[mb][0][2], s[mb][0][3])));
+    mx = fmaf(row_max(mx), mul, add);
+    if (__ballot(mx > m + kMaxSlack)) {
+      const float next = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= f;
+#pragma unroll
+      for (int b = 0; b < DB; ++b) acc[b][0] *= f;
+    }
+    const float sub = add - m;
+#pragma unroll
+    for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[mb][0][r], mul, sub));
+        l += p;
+        s[mb][0][r] = p;
+      }
+    if (masked && any_not_finite<T, DP, kFewKeys>(V, 0, lane)) {
+      accumulate_pairs<T, DP, 1, 2>(acc, s, V, 0, lane);
+      continue;
+    }
+    frag pf;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) pf[j] = (T)s[j >> 2][0][j & 3];
+#pragma unroll
+    for (int b = 0; b < DB; ++b) acc[b][0] = mma(acc[b][0], TL::col_frag(V, b, 0, lane), pf);
+  }
+  __builtin_amdgcn_s_waitcnt((0 << 8) | (7 << 4));
+  // join the wavefronts: each leaves its sums [16][DP] where its tiles were
+  l = row_sum(l);
+  float* own = reinterpret_cast<float*>(mine);
+#pragma unroll
+  for (int b = 0; b < DB; ++b) *reinterpret_cast<f32x4*>(own + l16 * DP + ((b * 4 + g) ^ (l16 & 7)) * 4) = acc[b][0];
+  if (g == 0) {
+    ml[wave][0][l16] = m;
+    ml[wave][1][l16] = l;
+  }
+  __syncthreads();
+  for (int e = tid; e < kFewRows * DP / 4; e += NW * 64) {
+    const int rr = e / (DP / 4), d4 = e % (DP / 4);
+    float mm = ml[0][0][rr], sum = 0.f;
+#pragma unroll
+    for (int w = 1; w < NW; ++w) mm = fmaxf(mm, ml[w][0][rr]);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml[w][0][rr] - mm);
+      sum += ml[w][1][rr] * f;
+      o += *reinterpret_cast<const f32x4*>(smem + w * 4 * kHalf + (rr * DP + (d4 ^ (rr & 7)) * 4) * 4) * f;
+    }
+    const int at = sp.tile * kFewRows + rr;
+    if (at >= rows) continue;
+    if (splits > 1) {
+      const size_t item = ((size_t)idx * a.kv_heads + kvh) * splits + split;
+      *reinterpret_cast<f32x4*>(part + (item * kFewRows + rr) * DP + d4 * 4) = o;
+      if (d4 == 0) {
+        part_ml[(item * kFewRows + rr) * 2] = mm;
+        part_ml[(item * kFewRows + rr) * 2 + 1] = sum;
+      }
+    } else {
+      const int qi = sp.q0 + at / group, hh = kvh * group + at % group;
+      if (d4 * 4 < a.d) store4(out + (long)qi * a.ld_o + hh * a.d + d4 * 4, o * (sum == 0.f ? 0.f : 1.f / sum));
+      if (d4 == 0) lse[(size_t)hh * a.rows_q + qi] = sum == 0.f ? kNegInf : (mm + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+  }
+}
+
+// Joins the splits of k_attend_few, in their order.  A thread takes four columns of a row.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int splits, const float* __restrict__ part, const float* __restrict__ part_ml,
+                                                     T* __restrict__ out, float* __restrict__ lse) {
+  const int group = a.heads / a.kv_heads, kvh = blockIdx.x % a.kv_heads, idx = blockIdx.x / a.kv_heads;
+  Span sp;
+  if (!find_span(a, idx, [group](int nq, int) { return (nq * group + kFewRows - 1) / kFewRows; }, sp)) return;
+  const size_t item = ((size_t)idx * a.kv_heads + kvh) * splits;
+  for (int e = threadIdx.x; e < kFewRows * DP / 4; e += 256) {
+    const int rr = e / (DP / 4), d4 = e % (DP / 4), at = sp.tile * kFewRows + rr;
+    if (at >= sp.nq * group || d4 * 4 >= a.d) continue;
+    float mm = kLowest, sum = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < splits; ++s) mm = fmaxf(mm, part_ml[((item + s) * kFewRows + rr) * 2]);
+    for (int s = 0; s < splits; ++s) {
+      const float f = __builtin_amdgcn_exp2f(part_ml[((item + s) * kFewRows + rr) * 2] - mm);
+      sum += part_ml[((item + s) * kFewRows + rr) * 2 + 1] * f;
+      o += *reinterpret_cast<const f32x4*>(part + ((item + s) * kFewRows + rr) * DP + d4 * 4) * f;
+    }
+    const int qi = sp.q0 + at / group, hh = kvh * group + at % group;
+    store4(out + (long)qi * a.ld_o + hh * a.d + d4 * 4, o * (sum == 0.f ? 0.f : 1.f / sum));
+    if (d4 == 0) lse[(size_t)hh * a.rows_q + qi] = sum == 0.f ? kNegInf : (mm + __builtin_amdgcn_logf(sum)) * kLn2;
+  }
+}
+
+// ---- backward -------------------------------------------------------------------------------------------------------------
+// Two kernels, each with sums of its own in registers and no atomics: k_attend_dq (a workgroup has queries, the keys pass by) and
+// k_attend_dkv (a workgroup has keys, the queries of all heads of the group pass by).  Scores and dP are formed in both: seven
+// products for the formula's five, instead of partial sums of dq in memory or atomics whose order changes results.
+
+// Bias gradient of a wavefront in LDS: sums of dS by r (as in the bias table), and 32 x 32 pairs at a time to sum along diagonals.
+template <int NB>
+struct BiasGrad {
+  static constexpr int kPairs = NB * 16 * 32;                                // floats
+  // dS of 32 keys (key 16 mb + 4 g + r of row nb * 16 + l16) into the buffer; row n holds its keys in chunks of four, swizzled.
+  static __device__ __forceinline__ void put(float* buf, const f32x4 (&ds)[2][NB], int lane) {
+    const int l16 = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int mb = 0; mb < 2; ++mb) {
+        const int n = nb * 16 + l16;
+        *reinterpret_cast<f32x4*>(buf + n * 32 + ((mb * 4 + g) ^ ((n >> 1) & 7)) * 4) = ds[mb][nb];
+      }
+  }
+  // Adds the diagonals to sums[]: key x of row n is r = x - n further right than sums' first.  A lane takes diagonal x = lane % 32
+  // and, where that leaves the block, diagonal x - 32; the halves of the wavefront take the odd and the even rows.
+  static __device__ __forceinline__ void diagonals(const float* buf, float* sums, int lane) {
+    const int x = lane & 31, half = lane >> 5;
+    float here = 0.f, wrapped = 0.f;
+#pragma unroll
+    for (int n2 = 0; n2 < NB * 8; ++n2) {
+      const int n = 2 * n2 + half, key = (x + n) & 31;
+      const float v = buf[n * 32 + (((key >> 2) ^ ((n >> 1) & 7)) << 2) + (key & 3)];
+      const bool in = x + n < 32;
+      here += in ? v : 0.f;
+      wrapped += in ? 0.f : v;
+    }
+    const float other = half ? here : wrapped;                               // what the partner lane keeps
+    const float got = __shfl_xor(other, 32);
+    // lanes 0..31 keep diagonal x, lanes 32..63 diagonal x - 32; even rows first in both
+    float* to = sums + (half ? x - 32 : x);
+    *to += half ? got + wrapped : here + got;
+  }
+};
+
+template <typename T, int DP, int NB, int NW, bool BIAS>
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttendArgs a, const T* __restrict__ q, const T* __restrict__ k,
+                                                      const T* __restrict__ v, const T* __restrict__ out, const float* __restrict__ lse,
+                                                      const T* __restrict__ dout, T* __restrict__ dq, float* __restrict__ stat,
+                                                      float* __restrict__ dbias_part, int want_dbias) {
+  typedef Tile<T, DP> TL;
+  typedef typename Frag<T>::type frag;
+  constexpr int KS = DP / 32, DB = DP / 16, ROWS = NW * NB * 16, NT = NW * 64;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
+  const int entries = BIAS ? bias_table_size(a.last) : 0;
+  float* table = reinterpret_cast<float*>(smem + 4 * TL::kBytes);
+  float* sums = table + ((entries + 3) & ~3) + wave * ((entries + 3) & ~3);
+  float* pairs = table + ((entries + 3) & ~3) * (NW + 1) + wave * BiasGrad<NB>::kPairs;
+  const HeadItem hi = head_item(a, blockIdx.x);
+  float* part = BIAS ? dbias_part + ((size_t)hi.idx * a.heads + hi.h) * a.buckets : nullptr;
+  Span sp;
+  if (!find_span(a, hi.idx, [](int nq, int) { return (nq + ROWS - 1) / ROWS; }, sp)) {
+    if (BIAS && want_dbias)
+      for (int b = tid; b < a.buckets; b += NT) part[b] = 0.f;
+    return;
+  }
+  const int i0 = (a.causal ? sp.tiles - 1 - sp.tile : sp.tile) * ROWS;
+  const int iw = i0 + wave * NB * 16, off = sp.nk - sp.nq;
+  const int kend = a.causal ? min(sp.nk, max(0, min(i0 + ROWS, sp.nq) + off)) : sp.nk;
+  const int tiles = (kend + kTileKeys - 1) / kTileKeys;
+  const T* kb_ = k + (long)sp.k0 * a.ld_k + hi.kvh * a.d;
+  const T* vb_ = v + (long)sp.k0 * a.ld_v + hi.kvh * a.d;
+  auto stage = [&](int t) {
+    unsigned char* to = smem + (t & 1) * 2 * TL::kBytes;
+    TL::template stage<kTileKeys, NT>(kb_ + (long)t * kTileKeys * a.ld_k, a.ld_k, sp.nk - t * kTileKeys, a.d, to, tid);
+    TL::template stage<kTileKeys, NT>(vb_ + (long)t * kTileKeys * a.ld_v, a.ld_v, sp.nk - t * kTileKeys, a.d, to + TL::kBytes, tid);
+  };
+  if (tiles > 0) stage(0);
+  float far_left = 0.f, far_right = 0.f, sum_left = 0.f, sum_right = 0.f;
+  if (BIAS) {
+    fill_bias_table<T, NT>(a, hi.h, table, tid);
+    if (want_dbias)
+      for (int e = lane; e < entries; e += 64) sums[e] = 0.f;
+    far_left = bias_value<T>(a, hi.h, a.side - 1);
+    far_right = a.causal ? 0.f : bias_value<T>(a, hi.h, 2 * a.side - 1);
+  }
+  frag qf[NB][KS], dof[NB][KS];
+  f32x4 acc[DB][NB];
+  float lse2[NB], delta[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int i = iw + nb * 16 + l16, row = sp.q0 + min(i, sp.nq - 1);
+    const bool in = i < sp.nq;
+    float dot = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[nb][ks] = load_frag<T>(q + (long)row * a.ld_q + hi.h * a.d, in, ks, g, a.d);
+      dof[nb][ks] = load_frag<T>(dout + (long)row * a.ld_do + hi.h * a.d, in, ks, g, a.d);
+      const frag of = load_frag<T>(out + (long)row * a.ld_o + hi.h * a.d, in, ks, g, a.d);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dot = fmaf(to_f32(dof[nb][ks][j]), to_f32(of[j]), dot);
+    }
+    delta[nb] = row_sum(dot);
+    const float e = lse[(size_t)hi.h * a.rows_q + row];
+    lse2[nb] = in && e != kNegInf ? e * kLog2e : __builtin_inff();          // a row that sees no key: P = 0
+    if (g == 0 && in) {
+      stat[(size_t)hi.h * a.rows_q + row] = lse2[nb];
+      stat[(size_t)(a.heads + hi.h) * a.rows_q + row] = delta[nb];
+    }
+#pragma unroll
+    for (int b = 0; b < DB; ++b) acc[b][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int lo = iw + off, top = lo + NB * 16 - 1;
+  for (int t = 0; t < tiles; ++t) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t + 1 < tiles) stage(t + 1);
+    const int kb = t * kTileKeys;
+    if (iw >= sp.nq || (a.causal && kb > top)) continue;
+    const unsigned char* K = smem + (t & 1) * 2 * TL::kBytes;
+    const unsigned char* V = K + TL::kBytes;
+    const bool masked = kb + kTileKeys > sp.nk || (a.causal && kb + kTileKeys - 1 > lo);
+    int side = 0;                                                            // -1, 1: all pairs in the last bucket of that side
+    if (BIAS) side = kb + kTileKeys - 1 - lo <= -a.last ? -1 : (kb - top >= a.last ? 1 : 0);
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2) {
+      f32x4 s[2][NB], dp[2][NB];
+#pragma unroll
+      for (int mb = 0; mb < 2; ++mb) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) s[mb][nb] = dp[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const frag kf = TL::row_frag(K, h2 * 2 + mb, ks, lane);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) s[mb][nb] = mma(s[mb][nb], kf, qf[nb][ks]);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const frag vf = TL::row_frag(V, h2 * 2 + mb, ks, lane);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) dp[mb][nb] = mma(dp[mb][nb], vf, dof[nb][ks]);
+        }
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float add = -lse2[nb];
+        const float* tb = table + kb + h2 * 32 + 4 * g - (lo + nb * 16 + l16) + a.last + kPad;
+        if (BIAS && side) add += side < 0 ? far_left : far_right;
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float x = add;
+            if (BIAS && !side) x += tb[mb * 16 + r];
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[mb][nb][r], a.c, x));
+            s[mb][nb][r] = p * (dp[mb][nb][r] - delta[nb]);
+          }
+        if (masked) {
+          const int end = a.causal ? min(sp.nk, lo + nb * 16 + l16 + 1) : sp.nk;
+#pragma unroll
+          for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (kb + h2 * 32 + mb * 16 + 4 * g + r >= end) s[mb][nb][r] = 0.f;
+        }
+      }
+      if (BIAS && want_dbias) {
+        if (side) {
+          float sum = 0.f;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int mb = 0; mb < 2; ++mb) sum += (s[mb][nb][0] + s[mb][nb][1]) + (s[mb][nb][2] + s[mb][nb][3]);
+          if (side < 0) sum_left += sum;
+          else sum_right += sum;
+        } else {
+          asm volatile("" ::: "memory");                                     // lanes read what other lanes of the wavefront wrote: in program order
+          BiasGrad<NB>::put(pairs, s, lane);
+          asm volatile("" ::: "memory");
+          BiasGrad<NB>::diagonals(pairs, sums + kb + h2 * 32 - lo + a.last + kPad, lane);
+        }
+      }
+      if (masked && any_not_finite<T, DP, 32>(K, h2 * 32, lane)) {
+        accumulate_pairs<T, DP, NB, 2>(acc, s, K, h2 * 32, lane);
+        continue;
+      }
+      frag df[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) df[nb][j] = (T)s[j >> 2][nb][j & 3];
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        const frag kf = TL::col_frag(K, b, h2, lane);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) acc[b][nb] = mma(acc[b][nb], kf, df[nb]);
+      }
+    }
+  }
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int i = iw + nb * 16 + l16;
+    if (i >= sp.nq) continue;
+    T* o = dq + (long)(sp.q0 + i) * a.ld_dq + hi.h * a.d;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+      if (b * 16 + 4 * g < a.d) store4(o + b * 16 + 4 * g, acc[b][nb] * a.scale);
+  }
+  if (BIAS && want_dbias) {                                                  // sums by r -> sums by bucket, in a fixed order
+    float* far_sums = reinterpret_cast<float*>(smem);                        // [2][NW], over the tiles
+    sum_left = wave_sum(sum_left);
+    sum_right = wave_sum(sum_right);
+    __syncthreads();
+    if (lane == 0) {
+      far_sums[wave] = sum_left;
+      far_sums[NW + wave] = sum_right;
+    }
+    __syncthreads();
+    const int pitch = (entries + 3) & ~3, mid = a.last + kPad;
+    const float* all = table + pitch;
+    for (int b = wave; b < a.buckets; b += NW) {
+      const bool right = b >= a.side;
+      const int n = right ? b - a.side : b;
+      const int from = n ? a.borders[n - 1] : (right ? 1 : 0), to = n < a.n_borders ? a.borders[n] : mid + 1;
+      float sum = 0.f;
+      for (int dist = from + lane; dist < to; dist += 64)
+#pragma unroll
+        for (int w = 0; w < NW; ++w) sum += all[w * pitch + mid + (right ? dist : -dist)];
+      sum = wave_sum(sum);
+      if (n == a.n_borders)
+#pragma unroll
+        for (int w = 0; w < NW; ++w) sum += far_sums[(right ? NW : 0) + w];
+      if (lane == 0) part[b] = sum;
+    }
+  }
+}
+
+// dbias[h][b] = sum over the items of their parts, in their order: 64 threads an entry.
+template <typename T>
+__global__ __launch_bounds__(64) void k_attend_dbias(int items, int entries, const float* __restrict__ part, T* __restrict__ dbias) {
+  const int e = blockIdx.x;
+  float sum = 0.f;
+  for (int i = threadIdx.x; i < items; i += 64) sum += part[(size_t)i * entries + e];
+  sum = wave_sum(sum);
+  if (threadIdx.x == 0) dbias[e] = from_f32<T>(sum);
+}
+
+// Keys' and values' gradients.  Workgroup: NW wavefronts of 16 NB keys of one key head; the queries of the group's heads pass by in
+// tiles of 64, Q and dO of two tiles in LDS with the rows' lse (base 2) and delta.
+template <typename T, int DP>
+constexpr int dkv_stage_bytes() { return 2 * Tile<T, DP>::kBytes + 2 * 64 * 4; }
+
+template <typename T, int DP, int NB, int NW, bool BIAS>
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(AttendArgs a, const T* __restrict__ q, const T* __restrict__ k,
+                                                       const T* __restrict__ v, const T* __restrict__ dout, const float* __restrict__ stat,
+                                                       T* __restrict__ dk, T* __restrict__ dv) {
+  typedef Tile<T, DP> TL;
+  typedef typename Frag<T>::type frag;
+  constexpr int KS = DP / 32, DB = DP / 16, ROWS = NW * NB * 16, NT = NW * 64, kStage = dkv_stage_bytes<T, DP>();
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  float* table = reinterpret_cast<float*>(smem + 2 * kStage);
+  const int group = a.heads / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
+  Span sp;
+  if (!find_span(a, blockIdx.x / a.kv_heads, [](int, int nk) { return (nk + ROWS - 1) / ROWS; }, sp)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
+  const int j0 = sp.tile * ROWS, jw = j0 + wave * NB * 16, jtop = jw + NB * 16 - 1, off = sp.nk - sp.nq;
+  const int first = a.causal ? max(0, j0 - off) / kTileKeys : 0, per = max(0, (sp.nq + kTileKeys - 1) / kTileKeys - first);
+  const int steps = per * group;
+  auto stage = [&](int it) {
+    const int h = kvh * group + it / per, r0 = (first + it % per) * kTileKeys, rows = sp.nq - r0;
+    unsigned char* to = smem + (it & 1) * kStage;
+    TL::template stage<kTileKeys, NT>(q + (long)(sp.q0 + r0) * a.ld_q + h * a.d, a.ld_q, rows, a.d, to, tid);
+    TL::template stage<kTileKeys, NT>(dout + (long)(sp.q0 + r0) * a.ld_do + h * a.d, a.ld_do, rows, a.d, to + TL::kBytes, tid);
+    if (wave < 2) {                                                          // lse by the first wavefront, delta by the second
+      const float* src = stat + (size_t)(wave * a.heads + h) * a.rows_q + sp.q0 + r0 + min(lane, rows - 1);
+      load4_to_lds(src, to + 2 * TL::kBytes + wave * 256);
+    }
+  };
+  if (steps > 0) stage(0);
+  frag kf[NB][KS], vf[NB][KS];
+  f32x4 ak[DB][NB], av[DB][NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int j = jw + nb * 16 + l16;
+    const long row = sp.k0 + min(j, sp.nk - 1);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kf[nb][ks] = load_frag<T>(k + row * a.ld_k + kvh * a.d, j < sp.nk, ks, g, a.d);
+      vf[nb][ks] = load_frag<T>(v + row * a.ld_v + kvh * a.d, j < sp.nk, ks, g, a.d);
+    }
+#pragma unroll
+    for (int b = 0; b < DB; ++b) ak[b][nb] = av[b][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  float far_left = 0.f, far_right = 0.f;
+  for (int it = 0; it < steps; ++it) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (BIAS && it % per == 0) {
+      const int h = kvh * group + it / per;
+      fill_bias_table<T, NT>(a, h, table, tid);
+      far_left = bias_value<T>(a, h, a.side - 1);
+      far_right = a.causal ? 0.f : bias_value<T>(a, h, 2 * a.side - 1);
+      __syncthreads();
+    }
+    if (it + 1 < steps) stage(it + 1);
+    const int qb = (first + it % per) * kTileKeys, lo = qb + off, top = lo + kTileKeys - 1;   // positions of the tile's queries
+    if (jw >= sp.nk || (a.causal && jw > top)) continue;
+    const unsigned char* Q = smem + (it & 1) * kStage;
+    const unsigned char* dO = Q + TL::kBytes;
+    const float* st = reinterpret_cast<const float*>(dO + TL::kBytes);
+    const bool masked = qb + kTileKeys > sp.nq || (a.causal && jtop > lo);
+    int side = 0;
+    if (BIAS) side = jtop - lo <= -a.last ? -1 : (jw - top >= a.last ? 1 : 0);
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2) {
+      f32x4 s[2][NB], dp[2][NB];
+#pragma unroll
+      for (int mb = 0; mb < 2; ++mb) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) s[mb][nb] = dp[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const frag qf = TL::row_frag(Q, h2 * 2 + mb, ks, lane);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) s[mb][nb] = mma(s[mb][nb], qf, kf[nb][ks]);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const frag of = TL::row_frag(dO, h2 * 2 + mb, ks, lane);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) dp[mb][nb] = mma(dp[mb][nb], of, vf[nb][ks]);
+        }
+      }
+      const float far = side < 0 ? far_left : far_right;
+#pragma unroll
+      for (int mb = 0; mb < 2; ++mb) {
+        const int row = (h2 * 2 + mb) * 16 + 4 * g;
+        const f32x4 e = *reinterpret_cast<const f32x4*>(st + row), dl = *reinterpret_cast<const f32x4*>(st + 64 + row);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const float* tb = table + jw + nb * 16 + l16 - (lo + row) + a.last + kPad;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float x = -e[r];
+            if (BIAS) x += side ? far : tb[-r];
+            float p = __builtin_amdgcn_exp2f(fmaf(s[mb][nb][r], a.c, x));
+            float ds = p * (dp[mb][nb][r] - dl[r]);
+            if (masked && (qb + row + r >= sp.nq || (a.causal && jw + nb * 16 + l16 > lo + row + r))) p = ds = 0.f;
+            s[mb][nb][r] = p;
+            dp[mb][nb][r] = ds;
+          }
+        }
+      }
+      if (masked && (any_not_finite<T, DP, 32>(dO, h2 * 32, lane) || any_not_finite<T, DP, 32>(Q, h2 * 32, lane))) {
+        accumulate_pairs<T, DP, NB, 2>(av, s, dO, h2 * 32, lane);
+        accumulate_pairs<T, DP, NB, 2>(ak, dp, Q, h2 * 32, lane);
+        continue;
+      }
+      frag pf[NB], df[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          pf[nb][j] = (T)s[j >> 2][nb][j & 3];
+          df[nb][j] = (T)dp[j >> 2][nb][j & 3];
+        }
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        const frag of = TL::col_frag(dO, b, h2, lane), qf = TL::col_frag(Q, b, h2, lane);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          av[b][nb] = mma(av[b][nb], of, pf[nb]);
+          ak[b][nb] = mma(ak[b][nb], qf, df[nb]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int j = jw + nb * 16 + l16;
+    if (j >= sp.nk) continue;
+    T* ok = dk + (long)(sp.k0 + j) * a.ld_dk + kvh * a.d;
+    T* ov = dv + (long)(sp.k0 + j) * a.ld_dv + kvh * a.d;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+      if (b * 16 + 4 * g < a.d) {
+        store4(ok + b * 16 + 4 * g, ak[b][nb] * a.scale);
+        store4(ov + b * 16 + 4 * g, av[b][nb]);
+      }
+  }
+}
+
+}  // namespace dchag

@@ -26,27 +26,6 @@
 
 namespace dchag {
 
-typedef const __attribute__((address_space(1))) void* gptr_t;
-typedef __attribute__((address_space(3))) void* lptr_t;
-
-// Wait until at most N vector-memory operations of this wavefront are outstanding
-// (gfx9 s_waitcnt immediate: vmcnt[3:0] | expcnt[6:4] | lgkmcnt[11:8] | vmcnt[5:4] at [15:14]).
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
-}
-
-// Each lane's 16 bytes of a wave-wide direct-to-LDS load land at lds_base + 16 * lane (lds_base is wave-uniform).
-// Written as an asm statement on purpose: the compiler files the builtin under "flat access that may touch LDS and
-// global memory", and while one is pending it turns every counted wait of the wavefront into a wait for zero, which
-// serialises the LDS fragment reads of the GEMM loops.  The kernels order these loads themselves (wait_vmcnt + barrier
-// before the stage is read; nothing outstanding when the block retires), so the compiler need not know them; the
-// memory clobber keeps it from moving LDS or global accesses across the statement.
-__device__ __forceinline__ void load16_to_lds(const void* src, void* lds_base) {
-  const unsigned lds_off = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(lptr_t)lds_base);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_off), "v"(src) : "memory", "m0");
-}
-
 // LDS stages hold rows of 64 bf16 (128 bytes = 8 chunks of 16 bytes).  Chunk c of row r sits at chunk
 // position c ^ ((r >> 1) & 7): the 16 consecutive rows a quarter-wavefront reads at one logical chunk
 // then fall into 16 different 16-byte bank groups (64 banks x 4 bytes), so ds_read_b128 is conflict-free.
@@ -540,12 +519,6 @@ struct CoreLane {
   // Wavefront w fills rows 16 w + 8 u + lane / 8 (u = 0, 1) of a RowOperand's slot; the byte of the chunk that belongs there:
   static __device__ __forceinline__ int ld_chunk(int lane, int u) { return ((lane & 7) ^ swz_chunk(u * 8 + (lane >> 3))) * 16; }
 };
-
-// 16 bytes a lane from base + voff (base wave-uniform) to lds_off + 16 * lane; an asm statement for the reason given at
-// load16_to_lds.
-__device__ __forceinline__ void load16_to_lds_at(const void* base, unsigned voff, unsigned lds_off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_off), "v"(voff), "s"(base) : "memory", "m0");
-}
 
 struct CoreFrags {
   bf16x8 a0[4][2], a1[4][2], bx[2][2], by[2][2];         // [block][k-step]; bx / by: B0 / B1 of an even slice, B1 / B0 of an odd one

@@ -8,7 +8,6 @@
 namespace dchag {
 
 constexpr int kBK = 64;       // K extent of one LDS stage (bf16 elements) = 8 chunks of 16 bytes
-constexpr int kXcds = 8;      // accelerator complex dies; workgroup ids go to them round-robin
 
 // LDS tiles are [rows][8 chunks] of 16-byte chunks (8 bf16).  The chunk index is XOR-ed with
 // low row bits so that the 32 rows a wavefront reads at one logical chunk spread over banks.

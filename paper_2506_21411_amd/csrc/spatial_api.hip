@@ -1,0 +1,395 @@
+// C ABI of the spatial block's operators: attention over packed sequences with its backward pass, and activations kept in 8 bits
+// with the weight gradient that reads them.  Argument validation, workspace layout and kernel launches.
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "host_base.h"
+#include "k_attend.h"
+#include "k_keep8.h"
+
+using namespace dchag;
+
+namespace {
+
+// ---- attention ------------------------------------------------------------------------------------------------------------
+int check_attention(dchag_dtype dt, const dchag_attention* a) {
+  if (dt != DCHAG_F32 && dt != DCHAG_BF16) return DCHAG_ERR_DTYPE;
+  if (!a || !a->q_starts || !a->k_starts) return DCHAG_ERR_NULL;
+  if (a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->heads > 4096) return DCHAG_ERR_SHAPE;
+  if (a->head_dim < 8 || a->head_dim > 128 || a->head_dim % 8) return DCHAG_ERR_SHAPE;
+  if (a->sequences < 0 || a->rows_q < 0 || a->rows_k < 0 || (a->causal != 0 && a->causal != 1)) return DCHAG_ERR_SHAPE;
+  if (!(a->scale >= 0.f) || !(a->scale < INFINITY)) return DCHAG_ERR_SHAPE;
+  const int64_t lds[8] = {a->ld_q, a->ld_k, a->ld_v, a->ld_out, a->ld_dout, a->ld_dq, a->ld_dk, a->ld_dv};
+  const int heads_of[8] = {a->heads, a->kv_heads, a->kv_heads, a->heads, a->heads, a->heads, a->kv_heads, a->kv_heads};
+  for (int i = 0; i < 8; ++i)
+    if (lds[i] != 0 && (lds[i] < (int64_t)heads_of[i] * a->head_dim || lds[i] % 8 || lds[i] > (1 << 23))) return DCHAG_ERR_SHAPE;
+  if (a->bias) {
+    if (!a->borders) return DCHAG_ERR_NULL;
+    if (a->n_borders < 1 || a->n_borders > kMaxBorders) return DCHAG_ERR_SHAPE;
+    for (int i = 0; i < a->n_borders; ++i)
+      if (a->borders[i] < 1 || a->borders[i] > kMaxDistance || (i && a->borders[i] <= a->borders[i - 1])) return DCHAG_ERR_SHAPE;
+    if (misaligned(a->bias)) return DCHAG_ERR_ALIGN;
+  }
+  if ((reinterpret_cast<uintptr_t>(a->q_starts) | reinterpret_cast<uintptr_t>(a->k_starts) | reinterpret_cast<uintptr_t>(a->k_used)) & 3u)
+    return DCHAG_ERR_ALIGN;
+  return DCHAG_OK;
+}
+
+AttendArgs kernel_args(const dchag_attention* a) {
+  AttendArgs k;
+  memset(&k, 0, sizeof k);
+  k.q_starts = a->q_starts;
+  k.k_starts = a->k_starts;
+  k.k_used = a->k_used;
+  k.sequences = a->sequences;
+  k.rows_q = a->rows_q;
+  k.rows_k = a->rows_k;
+  k.heads = a->heads;
+  k.kv_heads = a->kv_heads;
+  k.d = a->head_dim;
+  k.causal = a->causal;
+  const long dq = (long)a->heads * a->head_dim, dk = (long)a->kv_heads * a->head_dim;
+  k.ld_q = a->ld_q ? a->ld_q : dq;
+  k.ld_k = a->ld_k ? a->ld_k : dk;
+  k.ld_v = a->ld_v ? a->ld_v : dk;
+  k.ld_o = a->ld_out ? a->ld_out : dq;
+  k.ld_do = a->ld_dout ? a->ld_dout : dq;
+  k.ld_dq = a->ld_dq ? a->ld_dq : dq;
+  k.ld_dk = a->ld_dk ? a->ld_dk : dk;
+  k.ld_dv = a->ld_dv ? a->ld_dv : dk;
+  k.scale = a->scale > 0.f ? a->scale : 1.f / sqrtf((float)a->head_dim);
+  k.c = k.scale * kLog2e;
+  k.bias = a->bias;
+  if (a->bias) {
+    k.n_borders = a->n_borders;
+    k.last = a->borders[a->n_borders - 1];
+    k.side = a->n_borders + 1;
+    k.buckets = a->causal ? k.side : 2 * k.side;
+    memcpy(k.borders, a->borders, sizeof(int) * a->n_borders);
+  }
+  return k;
+}
+
+// Most tiles of `rows` rows that sequences of `total` rows can have.
+long tiles_bound(long total, long sequences, int rows) { return total / rows + std::min(sequences, total); }
+
+int padded_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+
+// How a forward call goes about its rows: few (k_attend_few, the keys dealt to `splits` workgroups) or tiles of 64 nb rows.
+struct ForwardPlan {
+  bool few;
+  int splits, nb;
+  long items;                 // row tiles at most
+  size_t part, part_ml, total;
+};
+ForwardPlan forward_plan(dchag_dtype dt, const AttendArgs& a) {
+  ForwardPlan p;
+  memset(&p, 0, sizeof p);
+  const int group = a.heads / a.kv_heads;
+  const long rows = (long)a.rows_q * group, seqs = std::min<long>(a.sequences, a.rows_q);
+  p.few = rows <= 32L * seqs;
+  p.splits = 1;
+  p.total = 256;
+  if (p.few) {
+    p.items = rows / kFewRows + std::min<long>(a.sequences, rows);
+    const int cus = compute_units();
+    const long base = p.items * a.kv_heads;
+    const long per_seq = a.rows_k / std::max(1, a.sequences);
+    if (base > 0) p.splits = (int)std::max(1L, std::min({3L * cus / base, per_seq / 256, 64L}));
+    if (p.splits > 1) {
+      const size_t n = (size_t)base * p.splits * kFewRows;
+      p.part = 0;
+      p.part_ml = align_up(n * padded_dim(a.d) * 4);
+      p.total = p.part_ml + align_up(n * 8);
+    }
+    return p;
+  }
+  p.nb = dt == DCHAG_BF16 && tiles_bound(a.rows_q, a.sequences, 128) * a.heads >= compute_units() ? 2 : 1;
+  p.items = tiles_bound(a.rows_q, a.sequences, p.nb * 64);
+  return p;
+}
+
+template <typename T, int DP, int NB, bool BIAS>
+int launch_attend(const AttendArgs& a, const ForwardPlan& p, const void* q, const void* k, const void* v, void* out, float* lse, hipStream_t st) {
+  constexpr int NW = 4;
+  const int lds = 4 * Tile<T, DP>::kBytes + (BIAS ? bias_table_size(a.last) * 4 : 0);
+  auto kern = k_attend<T, DP, NB, NW, BIAS>;
+  if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
+  StageTimer tm(DCHAG_STAGE_ATTEND, st);
+  kern<<<dim3((unsigned)(p.items * a.heads)), NW * 64, lds, st>>>(a, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v),
+                                                                  static_cast<T*>(out), lse);
+  return launch_status();
+}
+
+template <typename T, int DP, bool BIAS>
+int launch_few(const AttendArgs& a, const ForwardPlan& p, const void* q, const void* k, const void* v, void* out, float* lse, unsigned char* ws,
+               hipStream_t st) {
+  auto kern = k_attend_few<T, DP, BIAS>;
+  constexpr int lds = few_lds<T, DP>();
+  if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
+  float* part = reinterpret_cast<float*>(ws + p.part);
+  float* ml = reinterpret_cast<float*>(ws + p.part_ml);
+  {
+    StageTimer tm(DCHAG_STAGE_ATTEND, st);
+    kern<<<dim3((unsigned)(p.items * a.kv_heads * p.splits)), few_waves<T, DP>() * 64, lds, st>>>(
+        a, p.splits, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), lse, part, ml);
+  }
+  if (p.splits > 1) {
+    StageTimer tm(DCHAG_STAGE_ATTEND_JOIN, st);
+    k_attend_join<T, DP><<<dim3((unsigned)(p.items * a.kv_heads)), 256, 0, st>>>(a, p.splits, part, ml, static_cast<T*>(out), lse);
+  }
+  return launch_status();
+}
+
+template <typename T, int DP>
+int attend_dim(const AttendArgs& a, const ForwardPlan& p, const void* q, const void* k, const void* v, void* out, float* lse, unsigned char* ws,
+               hipStream_t st) {
+  if (p.few) return a.bias ? launch_few<T, DP, true>(a, p, q, k, v, out, lse, ws, st) : launch_few<T, DP, false>(a, p, q, k, v, out, lse, ws, st);
+  if constexpr (sizeof(T) == 2)
+    if (p.nb == 2) return a.bias ? launch_attend<T, DP, 2, true>(a, p, q, k, v, out, lse, st) : launch_attend<T, DP, 2, false>(a, p, q, k, v, out, lse, st);
+  return a.bias ? launch_attend<T, DP, 1, true>(a, p, q, k, v, out, lse, st) : launch_attend<T, DP, 1, false>(a, p, q, k, v, out, lse, st);
+}
+
+struct BackwardPlan {
+  int nb_q, nb_k;
+  long items_q, items_k;
+  size_t stat, dbias, total;
+};
+BackwardPlan backward_plan(dchag_dtype dt, const AttendArgs& a) {
+  BackwardPlan p;
+  p.nb_q = dt == DCHAG_BF16 && tiles_bound(a.rows_q, a.sequences, 128) * a.heads >= compute_units() ? 2 : 1;
+  p.nb_k = dt == DCHAG_BF16 && tiles_bound(a.rows_k, a.sequences, 128) * a.kv_heads >= compute_units() ? 2 : 1;
+  p.items_q = tiles_bound(a.rows_q, a.sequences, p.nb_q * 64);
+  p.items_k = tiles_bound(a.rows_k, a.sequences, p.nb_k * 64);
+  p.stat = 0;
+  p.dbias = align_up((size_t)2 * a.heads * a.rows_q * 4);
+  p.total = p.dbias + align_up((size_t)p.items_q * a.heads * a.buckets * 4) + 256;
+  return p;
+}
+
+struct BackwardPtrs {
+  const void *q, *k, *v, *out, *dout;
+  const float* lse;
+  void *dq, *dk, *dv, *dbias;
+};
+
+template <typename T, int DP, int NB, bool BIAS>
+int launch_dq(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
+  constexpr int NW = 4;
+  const int table = (bias_table_size(a.last) + 3) & ~3;
+  const int lds = 4 * Tile<T, DP>::kBytes + (BIAS ? table * 4 * (NW + 1) + NW * BiasGrad<NB>::kPairs * 4 : 0);
+  auto kern = k_attend_dq<T, DP, NB, NW, BIAS>;
+  if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
+  StageTimer tm(DCHAG_STAGE_BWD_ATTEND_QUERY, st);
+  if (p.items_q > 0)
+    kern<<<dim3((unsigned)(p.items_q * a.heads)), NW * 64, lds, st>>>(
+        a, static_cast<const T*>(t.q), static_cast<const T*>(t.k), static_cast<const T*>(t.v), static_cast<const T*>(t.out), t.lse,
+        static_cast<const T*>(t.dout), static_cast<T*>(t.dq), reinterpret_cast<float*>(ws + p.stat), reinterpret_cast<float*>(ws + p.dbias),
+        t.dbias != nullptr);
+  return launch_status();
+}
+template <typename T, int DP, int NB, bool BIAS>
+int launch_dkv(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
+  constexpr int NW = 4;
+  const int lds = 2 * dkv_stage_bytes<T, DP>() + (BIAS ? bias_table_size(a.last) * 4 : 0);
+  auto kern = k_attend_dkv<T, DP, NB, NW, BIAS>;
+  if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
+  StageTimer tm(DCHAG_STAGE_BWD_ATTEND_KEY, st);
+  if (p.items_k > 0)
+    kern<<<dim3((unsigned)(p.items_k * a.kv_heads)), NW * 64, lds, st>>>(
+        a, static_cast<const T*>(t.q), static_cast<const T*>(t.k), static_cast<const T*>(t.v), static_cast<const T*>(t.dout),
+        reinterpret_cast<const float*>(ws + p.stat), static_cast<T*>(t.dk), static_cast<T*>(t.dv));
+  return launch_status();
+}
+
+template <typename T, int DP, bool BIAS>
+int backward_bias(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
+  int rc;
+  if constexpr (sizeof(T) == 2) {
+    rc = p.nb_q == 2 ? launch_dq<T, DP, 2, BIAS>(a, p, t, ws, st) : launch_dq<T, DP, 1, BIAS>(a, p, t, ws, st);
+    if (!rc) rc = p.nb_k == 2 ? launch_dkv<T, DP, 2, BIAS>(a, p, t, ws, st) : launch_dkv<T, DP, 1, BIAS>(a, p, t, ws, st);
+  } else {
+    rc = launch_dq<T, DP, 1, BIAS>(a, p, t, ws, st);
+    if (!rc) rc = launch_dkv<T, DP, 1, BIAS>(a, p, t, ws, st);
+  }
+  if (rc || !BIAS || !t.dbias) return rc;
+  StageTimer tm(DCHAG_STAGE_BWD_ATTEND_BIAS, st);
+  const int entries = a.heads * a.buckets;
+  k_attend_dbias<T><<<dim3(entries), 64, 0, st>>>((int)p.items_q, entries, reinterpret_cast<const float*>(ws + p.dbias), static_cast<T*>(t.dbias));
+  return launch_status();
+}
+template <typename T, int DP>
+int backward_dim(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
+  return a.bias ? backward_bias<T, DP, true>(a, p, t, ws, st) : backward_bias<T, DP, false>(a, p, t, ws, st);
+}
+
+bool bad_workspace(const void* ws, size_t have, size_t need) {
+  return !ws || (reinterpret_cast<uintptr_t>(ws) & (kAlign - 1)) || have < need;
+}
+
+// ---- weight gradient from 8 bits ------------------------------------------------------------------------------------------
+struct GradPlan {
+  int tiles, splits, stretch;
+  size_t total;
+};
+GradPlan grad_plan(long rows, int d_out, int d_in) {
+  GradPlan p;
+  p.tiles = ((d_out + 127) / 128) * ((d_in + 127) / 128);
+  const long most = (rows + 255) / 256;                                      // a stretch of fewer rows costs more in partial sums than it gains
+  p.splits = (int)std::max(1L, std::min({2L * compute_units() / p.tiles, most, 64L}));
+  p.stretch = (int)(((rows + p.splits - 1) / p.splits + 63) / 64 * 64);
+  if (p.stretch < 64) p.stretch = 64;
+  p.splits = (int)std::max(1L, (rows + p.stretch - 1) / p.stretch);
+  p.total = p.splits > 1 ? align_up(((size_t)p.splits * d_out * d_in + (size_t)p.splits * d_out) * 4) : 256;
+  return p;
+}
+int check_rows8(dchag_dtype dt, int64_t rows, int D, int64_t ld) {
+  if (dt != DCHAG_F32 && dt != DCHAG_BF16) return DCHAG_ERR_DTYPE;
+  if (rows < 0 || D < 8 || D % 8 || D > (1 << 20) || (ld != 0 && (ld < D || ld % 8 || ld > (1 << 23)))) return DCHAG_ERR_SHAPE;
+  if (rows > (int64_t)0x7fffffff * 64 / ((D + 31) / 32)) return DCHAG_ERR_SHAPE;   // workgroups of 64 blocks
+  return DCHAG_OK;
+}
+int check_grad8(dchag_dtype dt, int rows, int d_out, int d_in, int64_t ld) {
+  if (dt != DCHAG_F32 && dt != DCHAG_BF16) return DCHAG_ERR_DTYPE;
+  if (rows < 0 || d_out < 8 || d_in < 8 || d_out % 8 || d_in % 8 || d_out > (1 << 20) || d_in > (1 << 20)) return DCHAG_ERR_SHAPE;
+  if (ld != 0 && (ld < d_out || ld % 8 || ld > (1 << 23))) return DCHAG_ERR_SHAPE;
+  if ((int64_t)((d_out + 127) / 128) * ((d_in + 127) / 128) > (1 << 20)) return DCHAG_ERR_SHAPE;
+  return DCHAG_OK;
+}
+
+template <typename T>
+int launch_grad8(const GradPlan& p, int rows, int d_out, int d_in, long ld, const void* dy, const void* codes, const void* scales, void* dW, void* db,
+                 float* part, hipStream_t st) {
+  auto kern = k_weight_grad8<T>;
+  constexpr int lds = 4 * Tile<T, 128>::kBytes;
+  if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
+  {
+    StageTimer tm(DCHAG_STAGE_WEIGHT_GRAD8, st);
+    kern<<<dim3((unsigned)(p.tiles * p.splits)), 256, lds, st>>>(rows, d_out, d_in, ld, p.stretch, static_cast<const T*>(dy),
+                                                               static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales),
+                                                               static_cast<T*>(dW), static_cast<T*>(db), p.splits > 1 ? part : nullptr);
+  }
+  if (p.splits > 1) {
+    StageTimer tm(DCHAG_STAGE_WEIGHT_GRAD8, st);
+    const size_t n = (size_t)d_out * d_in, all = n + d_out;
+    k_grad_join<T><<<dim3((unsigned)((all / 4 + 255) / 256)), 256, 0, st>>>(n, d_out, p.splits, part, static_cast<T*>(dW), static_cast<T*>(db));
+  }
+  return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dchag_attend_workspace_bytes(dchag_dtype dt, const dchag_attention* att, int which) {
+  if (check_attention(dt, att)) return 0;
+  const AttendArgs a = kernel_args(att);
+  if (which == 0) return forward_plan(dt, a).total;
+  if (which == 1) return backward_plan(dt, a).total;
+  return 0;
+}
+
+int dchag_attend(dchag_dtype dt, const dchag_attention* att, const void* q, const void* k, const void* v, void* out, float* lse, void* workspace,
+                 size_t workspace_bytes, void* stream) {
+  int rc = check_attention(dt, att);
+  if (rc) return rc;
+  const AttendArgs a = kernel_args(att);
+  if (a.rows_q > 0 && (!q || !out || !lse)) return DCHAG_ERR_NULL;
+  if (a.rows_q > 0 && a.rows_k > 0 && (!k || !v)) return DCHAG_ERR_NULL;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(lse)) return DCHAG_ERR_ALIGN;
+  const ForwardPlan p = forward_plan(dt, a);
+  if (bad_workspace(workspace, workspace_bytes, p.total)) return DCHAG_ERR_WORKSPACE;
+  if ((p.few ? p.items * a.kv_heads * p.splits : p.items * a.heads) > 0x7fffffffL) return DCHAG_ERR_SHAPE;
+  if (p.items == 0) return DCHAG_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  set_level(0);
+  const int dp = padded_dim(a.d);
+  if (dt == DCHAG_F32)
+    return dp == 32 ? attend_dim<float, 32>(a, p, q, k, v, out, lse, ws, st)
+         : dp == 64 ? attend_dim<float, 64>(a, p, q, k, v, out, lse, ws, st) : attend_dim<float, 128>(a, p, q, k, v, out, lse, ws, st);
+  return dp == 32 ? attend_dim<bf16, 32>(a, p, q, k, v, out, lse, ws, st)
+       : dp == 64 ? attend_dim<bf16, 64>(a, p, q, k, v, out, lse, ws, st) : attend_dim<bf16, 128>(a, p, q, k, v, out, lse, ws, st);
+}
+
+int dchag_attend_backward(dchag_dtype dt, const dchag_attention* att, const void* q, const void* k, const void* v, const void* out, const float* lse,
+                          const void* dout, void* dq, void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_attention(dt, att);
+  if (rc) return rc;
+  const AttendArgs a = kernel_args(att);
+  if (a.rows_q > 0 && (!q || !out || !lse || !dout || !dq)) return DCHAG_ERR_NULL;
+  if (a.rows_k > 0 && (!k || !v || !dk || !dv)) return DCHAG_ERR_NULL;
+  if (dbias && !att->bias) return DCHAG_ERR_SHAPE;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(lse) || misaligned(dout) || misaligned(dq) || misaligned(dk) ||
+      misaligned(dv) || misaligned(dbias))
+    return DCHAG_ERR_ALIGN;
+  const BackwardPlan p = backward_plan(dt, a);
+  if (bad_workspace(workspace, workspace_bytes, p.total)) return DCHAG_ERR_WORKSPACE;
+  if (p.items_q * a.heads > 0x7fffffffL || p.items_k * a.kv_heads > 0x7fffffffL) return DCHAG_ERR_SHAPE;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  const BackwardPtrs t{q, k, v, out, dout, lse, dq, dk, dv, dbias};
+  set_level(0);
+  const int dp = padded_dim(a.d);
+  if (dt == DCHAG_F32)
+    return dp == 32 ? backward_dim<float, 32>(a, p, t, ws, st) : dp == 64 ? backward_dim<float, 64>(a, p, t, ws, st) : backward_dim<float, 128>(a, p, t, ws, st);
+  return dp == 32 ? backward_dim<bf16, 32>(a, p, t, ws, st) : dp == 64 ? backward_dim<bf16, 64>(a, p, t, ws, st) : backward_dim<bf16, 128>(a, p, t, ws, st);
+}
+
+int dchag_pack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void* x, void* codes, void* scales, void* stream) {
+  int rc = check_rows8(dt, rows, D, ld);
+  if (rc) return rc;
+  if (rows == 0) return DCHAG_OK;
+  if (!x || !codes || !scales) return DCHAG_ERR_NULL;
+  if (misaligned(x) || misaligned(codes) || misaligned(scales)) return DCHAG_ERR_ALIGN;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const long groups = (rows * ((D + 31) / 32) + 63) / 64;
+  set_level(0);
+  StageTimer tm(DCHAG_STAGE_PACK8, st);
+  if (dt == DCHAG_F32)
+    k_pack8<float><<<dim3((unsigned)groups), 256, 0, st>>>(rows, D, ld ? ld : D, static_cast<const float*>(x), static_cast<unsigned char*>(codes), static_cast<unsigned char*>(scales));
+  else
+    k_pack8<bf16><<<dim3((unsigned)groups), 256, 0, st>>>(rows, D, ld ? ld : D, static_cast<const bf16*>(x), static_cast<unsigned char*>(codes), static_cast<unsigned char*>(scales));
+  return launch_status();
+}
+
+int dchag_unpack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void* codes, const void* scales, void* x, void* stream) {
+  int rc = check_rows8(dt, rows, D, ld);
+  if (rc) return rc;
+  if (rows == 0) return DCHAG_OK;
+  if (!x || !codes || !scales) return DCHAG_ERR_NULL;
+  if (misaligned(x) || misaligned(codes) || misaligned(scales)) return DCHAG_ERR_ALIGN;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const long groups = (rows * ((D + 31) / 32) + 63) / 64;
+  set_level(0);
+  StageTimer tm(DCHAG_STAGE_UNPACK8, st);
+  if (dt == DCHAG_F32)
+    k_unpack8<float><<<dim3((unsigned)groups), 256, 0, st>>>(rows, D, ld ? ld : D, static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales), static_cast<float*>(x));
+  else
+    k_unpack8<bf16><<<dim3((unsigned)groups), 256, 0, st>>>(rows, D, ld ? ld : D, static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales), static_cast<bf16*>(x));
+  return launch_status();
+}
+
+size_t dchag_weight_grad8_workspace_bytes(dchag_dtype dt, int rows, int d_out, int d_in) {
+  if (check_grad8(dt, rows, d_out, d_in, 0)) return 0;
+  return grad_plan(rows, d_out, d_in).total;
+}
+
+int dchag_weight_grad8(dchag_dtype dt, int rows, int d_out, int d_in, int64_t ld, const void* dy, const void* codes, const void* scales, void* dW,
+                       void* db, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_grad8(dt, rows, d_out, d_in, ld);
+  if (rc) return rc;
+  if (!dW || (rows > 0 && (!dy || !codes || !scales))) return DCHAG_ERR_NULL;
+  if (misaligned(dy) || misaligned(codes) || misaligned(scales) || misaligned(dW) || misaligned(db)) return DCHAG_ERR_ALIGN;
+  const GradPlan p = grad_plan(rows, d_out, d_in);
+  if (bad_workspace(workspace, workspace_bytes, p.total)) return DCHAG_ERR_WORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  set_level(0);
+  float* part = static_cast<float*>(workspace);
+  if (dt == DCHAG_F32) return launch_grad8<float>(p, rows, d_out, d_in, ld ? ld : d_out, dy, codes, scales, dW, db, part, st);
+  return launch_grad8<bf16>(p, rows, d_out, d_in, ld ? ld : d_out, dy, codes, scales, dW, db, part, st);
+}
+
+}  // extern "C"
