@@ -459,57 +459,66 @@ def log_borders(buckets: int, max_distance: int) -> List[int]:
     return out
 
 
-def _rows_of(t: torch.Tensor, name: str, heads: Optional[int] = None, d: Optional[int] = None) -> int:
+def _row_stride(t: torch.Tensor, name: str) -> int:
     """Elements from one row to the next of [rows, heads, d] whose heads lie one behind the other."""
-    if t.dim() != 3 or (heads is not None and (t.shape[1], t.shape[2]) != (heads, d)):
-        raise ValueError(f"{name} must be [rows, heads, head_dim]" + (f" with {heads} heads of {d}" if heads is not None else ""))
-    if t.numel() and ((t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+    rows, heads, d = t.shape
+    row, head, one = t.stride()
+    if t.numel() and ((d > 1 and one != 1) or (heads > 1 and head != d)):
         raise ValueError(f"the heads of a row of {name} must lie one behind the other")
-    return int(t.stride(0)) if t.shape[0] > 1 else 0
+    return row if rows > 1 else 0
 
 
-def _dev_ptr(t: Optional[torch.Tensor], like: Optional[torch.Tensor], name: str, dtype: Optional[torch.dtype] = None):
-    """Address of a tensor on the current device, of the given dtype or like's; its strides are the caller's business."""
-    if t is None:
-        return None
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+def _addr(t: torch.Tensor, dtype: torch.dtype, device: int, name: str) -> int:
+    """Address of a tensor of that type on the current device; its strides are the caller's business."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if not t.is_cuda or t.device.index != device:
         raise ValueError(f"{name} must be a tensor on the current device")
-    if t.dtype != (like.dtype if dtype is None else dtype):
-        raise TypeError(f"{name} must be {like.dtype if dtype is None else dtype}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-def _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders):
+def _vector(t: torch.Tensor, n: int, name: str) -> None:
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous vector of {n}")
+
+
+def _device(t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the current device")
+    return torch.cuda.current_device()
+
+
+def _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders, device):
     """The C struct of a call, and what it points to on the host."""
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("q, k and v must be [rows, heads, head_dim]")
-    heads, d, kv_heads = q.shape[1], q.shape[2], k.shape[1]
+    if q.dim() != 3 or k.dim() != 3 or v.shape != k.shape:
+        raise ValueError("q must be [rows, heads, head_dim], k and v [rows, kv_heads, head_dim]")
+    rows_q, heads, d = q.shape
+    rows_k, kv_heads, dk = k.shape
+    if dk != d:
+        raise ValueError("q, k and v must have heads of one size")
+    if q_starts.dim() != 1 or q_starts.shape[0] < 1:
+        raise ValueError("q_starts must be a vector of one entry more than there are sequences")
+    sequences = q_starts.shape[0] - 1
+    _vector(q_starts, sequences + 1, "q_starts")
+    _vector(k_starts, sequences + 1, "k_starts")
     a = _CAttention()
-    a.heads, a.kv_heads, a.head_dim, a.causal = heads, kv_heads, d, int(bool(causal))
-    a.rows_q, a.rows_k, a.scale = q.shape[0], k.shape[0], float(scale)
-    if v.shape != k.shape:
-        raise ValueError("k and v must have the same shape")
-    a.ld_q, a.ld_k, a.ld_v = _rows_of(q, "q"), _rows_of(k, "k", kv_heads, d), _rows_of(v, "v", kv_heads, d)
-    for name, t, n in (("q_starts", q_starts, None), ("k_starts", k_starts, 0), ("k_used", k_used, -1)):
-        if t is None:
-            continue
-        if t.dim() != 1 or not t.is_contiguous() or t.numel() < 1 - (n == -1):
-            raise ValueError(f"{name} must be a contiguous vector")
-        if n is not None and t.numel() != q_starts.numel() + n:
-            raise ValueError(f"{name} does not have as many sequences as q_starts")
-    a.sequences = q_starts.numel() - 1
-    a.q_starts = _dev_ptr(q_starts, None, "q_starts", torch.int32)
-    a.k_starts = _dev_ptr(k_starts, None, "k_starts", torch.int32)
-    a.k_used = _dev_ptr(k_used, None, "k_used", torch.int32)
-    host = None
+    a.heads, a.kv_heads, a.head_dim, a.causal, a.sequences = heads, kv_heads, d, 1 if causal else 0, sequences
+    a.rows_q, a.rows_k, a.scale = rows_q, rows_k, scale
+    a.ld_q, a.ld_k, a.ld_v = _row_stride(q, "q"), _row_stride(k, "k"), _row_stride(v, "v")
+    a.q_starts = _addr(q_starts, torch.int32, device, "q_starts")
+    a.k_starts = _addr(k_starts, torch.int32, device, "k_starts")
+    if k_used is not None:
+        _vector(k_used, sequences, "k_used")
+        a.k_used = _addr(k_used, torch.int32, device, "k_used")
     if (bias is None) != (borders is None):
         raise ValueError("bias and borders come together")
-    if bias is not None:
-        host = (ctypes.c_int32 * max(1, len(borders)))(*[int(b) for b in borders])
-        if tuple(bias.shape) != (heads, (len(borders) + 1) * (1 if causal else 2)) or not bias.is_contiguous():
-            raise ValueError("bias must be contiguous, [heads, buckets] with one bucket more than borders, twice as many if not causal")
-        a.bias, a.n_borders = _dev_ptr(bias, q, "bias"), len(borders)
-        a.borders = ctypes.cast(host, ctypes.c_void_p)
+    if bias is None:
+        return a, None
+    n = len(borders)
+    if tuple(bias.shape) != (heads, (n + 1) * (1 if causal else 2)) or not bias.is_contiguous():
+        raise ValueError("bias must be contiguous, [heads, buckets] with one bucket more than borders, twice as many if not causal")
+    host = (ctypes.c_int32 * max(1, n))(*borders)
+    a.bias, a.n_borders, a.borders = _addr(bias, q.dtype, device, "bias"), n, ctypes.addressof(host)
     return a, host
 
 
@@ -521,20 +530,24 @@ def dchag_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: to
     """(out [rows_q, heads, d], lse [heads, rows_q] float32) of attention over packed sequences: q [rows_q, heads, d], k and v
     [rows_k, kv_heads, d], int32 starts [sequences + 1] on the device.  Rows of a tensor may have gaps between them (columns of a
     joint projection).  Rows of no sequence are not written: give an `out` of your own if they are read later."""
-    a, host = _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders)
-    dt, lib = _dt(q), load_library()
+    device = _device(q)
+    a, host = _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders, device)
+    dt, dtype, lib = _dt(q), q.dtype, load_library()
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    a.ld_out = _rows_of(out, "out", q.shape[1], q.shape[2])
+        out = torch.empty(q.shape, dtype=dtype, device=q.device)
+    else:
+        if out.shape != q.shape:
+            raise ValueError("out must be shaped like q")
+        a.ld_out = _row_stride(out, "out")
     if lse is None:
-        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-    if out.shape != q.shape or tuple(lse.shape) != (q.shape[1], q.shape[0]) or not lse.is_contiguous():
-        raise ValueError("out must be shaped like q, lse [heads, rows_q] and contiguous")
+        lse = torch.empty((a.heads, a.rows_q), dtype=torch.float32, device=q.device)
+    elif tuple(lse.shape) != (a.heads, a.rows_q) or not lse.is_contiguous():
+        raise ValueError("lse must be [heads, rows_q] and contiguous")
     if workspace is None:
-        workspace = _workspace(lib.dchag_attend_workspace_bytes(dt, ctypes.byref(a), 0), q.device)
-    _check(lib.dchag_attend(dt, ctypes.byref(a), _dev_ptr(q, q, "q"), _dev_ptr(k, q, "k"), _dev_ptr(v, q, "v"),
-                            _dev_ptr(out, q, "out"), _dev_ptr(lse, None, "lse", torch.float32),
-                            ctypes.c_void_p(workspace.data_ptr()), workspace.numel(), _stream(stream)))
+        workspace = _workspace(lib.dchag_attend_workspace_bytes(dt, a, 0), q.device)
+    _check(lib.dchag_attend(dt, a, _addr(q, dtype, device, "q"), _addr(k, dtype, device, "k"), _addr(v, dtype, device, "v"),
+                            _addr(out, dtype, device, "out"), _addr(lse, torch.float32, device, "lse"), workspace.data_ptr(),
+                            workspace.numel(), _stream(stream)))
     return out, lse
 
 
@@ -547,30 +560,32 @@ def dchag_attend_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out
                           workspace: Optional[torch.Tensor] = None, stream=None):
     """(dq, dk, dv, dbias or None) of <dout, dchag_attend(...)>; out and lse are those of the forward call with the same arguments.
     Rows of no sequence are not written."""
-    a, host = _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders)
-    dt, lib = _dt(q), load_library()
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
-    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
-    if bias is None and dbias is not None:
-        raise ValueError("dbias without a bias")
-    if bias is not None and want_dbias and dbias is None:
-        dbias = torch.empty_like(bias)
-    if dbias is not None and (dbias.shape != bias.shape or not dbias.is_contiguous()):
-        raise ValueError("dbias must be shaped like bias and contiguous")
-    for name, t, like in (("out", out, q), ("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
-        if t.shape != like.shape:
-            raise ValueError(f"{name} must be shaped like {'q' if like is q else 'k and v'}")
-        setattr(a, "ld_" + name, _rows_of(t, name))
-    if tuple(lse.shape) != (q.shape[1], q.shape[0]) or not lse.is_contiguous():
+    device = _device(q)
+    a, host = _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders, device)
+    dt, dtype, lib = _dt(q), q.dtype, load_library()
+    if dq is None:
+        dq = torch.empty(q.shape, dtype=dtype, device=q.device)
+    if dk is None:
+        dk = torch.empty(k.shape, dtype=dtype, device=q.device)
+    if dv is None:
+        dv = torch.empty(k.shape, dtype=dtype, device=q.device)
+    if dbias is None and bias is not None and want_dbias:
+        dbias = torch.empty(bias.shape, dtype=dtype, device=q.device)
+    if dbias is not None and (bias is None or dbias.shape != bias.shape or not dbias.is_contiguous()):
+        raise ValueError("dbias goes with a bias, is shaped like it and contiguous")
+    if out.shape != q.shape or dout.shape != q.shape or dq.shape != q.shape or dk.shape != k.shape or dv.shape != k.shape:
+        raise ValueError("out, dout and dq must be shaped like q, dk and dv like k")
+    if tuple(lse.shape) != (a.heads, a.rows_q) or not lse.is_contiguous():
         raise ValueError("lse must be [heads, rows_q] and contiguous")
+    a.ld_out, a.ld_dout, a.ld_dq = _row_stride(out, "out"), _row_stride(dout, "dout"), _row_stride(dq, "dq")
+    a.ld_dk, a.ld_dv = _row_stride(dk, "dk"), _row_stride(dv, "dv")
     if workspace is None:
-        workspace = _workspace(lib.dchag_attend_workspace_bytes(dt, ctypes.byref(a), 1), q.device)
-    ptrs = [_dev_ptr(t, q, n) for n, t in (("q", q), ("k", k), ("v", v), ("out", out))]
-    ptrs += [_dev_ptr(lse, None, "lse", torch.float32)]
-    ptrs += [_dev_ptr(t, q, n) for n, t in (("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv), ("dbias", dbias))]
-    _check(lib.dchag_attend_backward(dt, ctypes.byref(a), *ptrs, ctypes.c_void_p(workspace.data_ptr()), workspace.numel(),
-                                     _stream(stream)))
+        workspace = _workspace(lib.dchag_attend_workspace_bytes(dt, a, 1), q.device)
+    _check(lib.dchag_attend_backward(
+        dt, a, _addr(q, dtype, device, "q"), _addr(k, dtype, device, "k"), _addr(v, dtype, device, "v"), _addr(out, dtype, device, "out"),
+        _addr(lse, torch.float32, device, "lse"), _addr(dout, dtype, device, "dout"), _addr(dq, dtype, device, "dq"),
+        _addr(dk, dtype, device, "dk"), _addr(dv, dtype, device, "dv"), None if dbias is None else _addr(dbias, dtype, device, "dbias"),
+        workspace.data_ptr(), workspace.numel(), _stream(stream)))
     return dq, dk, dv, dbias
 
 
@@ -588,25 +603,28 @@ def _codes8(codes: torch.Tensor, scales: torch.Tensor, rows: int, D: int) -> Non
 
 def dchag_pack8(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """(codes uint8 [rows, D], scales uint8 [rows, (D + 31) // 32]): the rows of x in 8 bits, one exponent for every 32 values."""
-    ld, (rows, D) = _matrix(x, "x"), x.shape
-    codes = torch.empty((rows, D), dtype=torch.uint8, device=x.device) if codes is None else codes
-    scales = torch.empty((rows, (D + 31) // 32), dtype=torch.uint8, device=x.device) if scales is None else scales
+    ld, (rows, D), device = _matrix(x, "x"), x.shape, _device(x)
+    if codes is None:
+        codes = torch.empty((rows, D), dtype=torch.uint8, device=x.device)
+    if scales is None:
+        scales = torch.empty((rows, (D + 31) // 32), dtype=torch.uint8, device=x.device)
     _codes8(codes, scales, rows, D)
-    _check(load_library().dchag_pack8(_dt(x), rows, D, ld, _dev_ptr(x, x, "x"), _dev_ptr(codes, None, "codes", torch.uint8),
-                                      _dev_ptr(scales, None, "scales", torch.uint8), _stream(stream)))
+    _check(load_library().dchag_pack8(_dt(x), rows, D, ld, _addr(x, x.dtype, device, "x"), _addr(codes, torch.uint8, device, "codes"),
+                                      _addr(scales, torch.uint8, device, "scales"), _stream(stream)))
     return codes, scales
 
 
 def dchag_unpack8(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
                   out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The rows that codes and scales (dchag_pack8) stand for."""
-    rows, D = codes.shape
+    (rows, D), device = codes.shape, _device(codes)
     _codes8(codes, scales, rows, D)
-    out = torch.empty((rows, D), dtype=dtype, device=codes.device) if out is None else out
-    if tuple(out.shape) != (rows, D):
+    if out is None:
+        out = torch.empty((rows, D), dtype=dtype, device=codes.device)
+    elif tuple(out.shape) != (rows, D):
         raise ValueError("out must be [rows, D]")
-    _check(load_library().dchag_unpack8(_dt(out), rows, D, _matrix(out, "out"), _dev_ptr(codes, None, "codes", torch.uint8),
-                                        _dev_ptr(scales, None, "scales", torch.uint8), _dev_ptr(out, out, "out"), _stream(stream)))
+    _check(load_library().dchag_unpack8(_dt(out), rows, D, _matrix(out, "out"), _addr(codes, torch.uint8, device, "codes"),
+                                        _addr(scales, torch.uint8, device, "scales"), _addr(out, out.dtype, device, "out"), _stream(stream)))
     return out
 
 
@@ -615,17 +633,19 @@ def dchag_weight_grad8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tens
     """(dW [d_out, d_in], db [d_out] or None) of a linear layer: dy [rows, d_out], its input in 8 bits (dchag_pack8)."""
     ld, (rows, d_out), d_in = _matrix(dy, "dy"), dy.shape, codes.shape[-1]
     _codes8(codes, scales, rows, d_in)
-    dW = torch.empty((d_out, d_in), dtype=dy.dtype, device=dy.device) if dW is None else dW
-    db = torch.empty((d_out,), dtype=dy.dtype, device=dy.device) if db is None and want_db else db
-    if tuple(dW.shape) != (d_out, d_in) or (db is not None and tuple(db.shape) != (d_out,)):
-        raise ValueError("dW must be [d_out, d_in], db [d_out]")
+    device, dtype = _device(dy), dy.dtype
+    if dW is None:
+        dW = torch.empty((d_out, d_in), dtype=dtype, device=dy.device)
+    if db is None and want_db:
+        db = torch.empty((d_out,), dtype=dtype, device=dy.device)
+    if tuple(dW.shape) != (d_out, d_in) or not dW.is_contiguous() or (db is not None and (tuple(db.shape) != (d_out,) or not db.is_contiguous())):
+        raise ValueError("dW must be [d_out, d_in], db [d_out], contiguous")
     dt, lib = _dt(dy), load_library()
     if workspace is None:
         workspace = _workspace(lib.dchag_weight_grad8_workspace_bytes(dt, rows, d_out, d_in), dy.device)
-    _dev_ptr(dW, dy, "dW"), _dev_ptr(db, dy, "db")
-    _check(lib.dchag_weight_grad8(dt, rows, d_out, d_in, ld, _dev_ptr(dy, dy, "dy"), _dev_ptr(codes, None, "codes", torch.uint8),
-                                  _dev_ptr(scales, None, "scales", torch.uint8), _ptr(dW, dy), _ptr(db, dy),
-                                  ctypes.c_void_p(workspace.data_ptr()), workspace.numel(), _stream(stream)))
+    _check(lib.dchag_weight_grad8(dt, rows, d_out, d_in, ld, _addr(dy, dtype, device, "dy"), _addr(codes, torch.uint8, device, "codes"),
+                                  _addr(scales, torch.uint8, device, "scales"), _addr(dW, dtype, device, "dW"),
+                                  None if db is None else _addr(db, dtype, device, "db"), workspace.data_ptr(), workspace.numel(), _stream(stream)))
     return dW, db
 
 

@@ -16,6 +16,8 @@
 // a lane, and two such blocks are, without any exchange, the operand of the next product over 32 tile rows in the order
 // {4 g + 0..3, 16 + 4 g + 0..3}, g = l / 16; the other operand is read from LDS in the same order (transposing reads).
 #pragma once
+#include <type_traits>
+
 #include "dchag_dev.h"
 
 namespace dchag {
@@ -101,9 +103,15 @@ struct Tile {
       return r;
     }
   }
-  // Element col of a row.
-  static __device__ __forceinline__ float at(const unsigned char* t, int row, int col) {
-    return to_f32(*reinterpret_cast<const T*>(t + row * kPitch + ((col / kElems) ^ swz(row)) * 16 + (col % kElems) * (int)sizeof(T)));
+  // Elements col .. col + 3 of a row; col a multiple of 4.
+  static __device__ __forceinline__ f32x4 four(const unsigned char* t, int row, int col) {
+    const unsigned char* p = t + row * kPitch + ((col / kElems) ^ swz(row)) * 16 + (col % kElems) * (int)sizeof(T);
+    if constexpr (sizeof(T) == 2) {
+      const bf16x4 v = *reinterpret_cast<const bf16x4*>(p);
+      return f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+    } else {
+      return *reinterpret_cast<const f32x4*>(p);
+    }
   }
   // Fills ROWS rows of a tile from rows base + row * ld (direct-to-LDS loads; NT threads take part, tid among them); rows from
   // `rows` on and columns from d on come from zeros, so nothing outside the sequence and the head is read.
@@ -113,10 +121,13 @@ struct Tile {
     static_assert(kLoads * NT == ROWS * kChunks, "rows do not split over the threads");
     if (rows >= ROWS && d == DP) {
       const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(lptr_t)(lds + (tid & ~63) * 16));
+      const uint64_t at = reinterpret_cast<uint64_t>(base);                   // the same in every lane, which the compiler does not always see
+      const unsigned low = __builtin_amdgcn_readfirstlane((unsigned)at), high = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32));
+      const void* first = reinterpret_cast<const void*>((uint64_t)high << 32 | low);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int idx = i * NT + tid, row = idx / kChunks, chunk = (idx % kChunks) ^ swz(row);
-        load16_to_lds_at(base, (unsigned)(row * (int)ld * (int)sizeof(T) + chunk * 16), lds0 + i * NT * 16);
+        load16_to_lds_at(first, (unsigned)(row * (int)ld * (int)sizeof(T) + chunk * 16), __builtin_amdgcn_readfirstlane(lds0 + i * NT * 16));
       }
     } else {
 #pragma unroll
@@ -168,11 +179,13 @@ __device__ __forceinline__ LanePair pair16(float v) {
   const unsigned u = __builtin_bit_cast(unsigned, v);
   return lane_pair(__builtin_amdgcn_permlane16_swap(u, u, false, false));
 }
+// The larger of two numbers, NaN if one is (fmaxf would first quiet every operand, an instruction each).
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 // Maximum and sum over the four lanes of a row (lane, lane ^ 16, lane ^ 32, lane ^ 48); every one of them gets it.
 __device__ __forceinline__ float row_max(float v) {
   LanePair p = pair32(v);
-  p = pair16(fmaxf(p.low, p.high));
-  return fmaxf(p.low, p.high);
+  p = pair16(larger(p.low, p.high));
+  return larger(p.low, p.high);
 }
 __device__ __forceinline__ float row_sum(float v) {
   LanePair p = pair32(v);
@@ -258,27 +271,31 @@ __device__ __forceinline__ void fill_bias_table(const AttendArgs& a, int h, floa
   for (int i = tid; i < n; i += NT) table[i] = bias_value<T>(a, h, bucket_of(a, i - mid));
 }
 
-// Adds p v to acc pair by pair, leaving out the pairs with p = 0: what a masked pair's v holds then does not matter, not even a
-// NaN.  For tiles with masked pairs and with values that are not finite; acc and p as in the products over a tile of 64 rows.
-template <typename T, int DP, int NB, int MB>
-__device__ __forceinline__ void accumulate_pairs(f32x4 (&acc)[DP / 16][NB], const f32x4 (&p)[MB][NB], const unsigned char* t, int row0, int lane) {
+// acc += p v over the 32 rows row0 .. of a tile, as mma(acc, column fragments, p) does but pair by pair, leaving out the pairs with p = 0:
+// what a masked pair's v holds then does not matter, not even a NaN.  For tiles with masked pairs and with values that are not finite.
+template <typename T, int DP, int NB>
+__device__ __forceinline__ void accumulate_pairs(f32x4 (&acc)[DP / 16][NB], const typename Frag<T>::type (&p)[NB], const unsigned char* t, int row0, int lane) {
   const int l16 = lane & 15, g = lane >> 4;
 #pragma unroll 1
-  for (int j = 0; j < MB * 16; ++j) {
+  for (int j = 0; j < 32; ++j) {
+    float w[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       float own = 0.f;
 #pragma unroll
-      for (int m = 0; m < MB * 4; ++m)
-        if (m == (j >> 4) * 4 + (j & 3)) own = p[m >> 2][nb][m & 3];
-      const float w = __shfl(own, l16 + 16 * ((j >> 2) & 3));
+      for (int m = 0; m < 8; ++m)
+        if (m == (j >> 4) * 4 + (j & 3)) own = to_f32(p[nb][m]);
+      w[nb] = __shfl(own, l16 + 16 * ((j >> 2) & 3));
+    }
 #pragma unroll
-      for (int b = 0; b < DP / 16; ++b)
+    for (int b = 0; b < DP / 16; ++b) {
+      const f32x4 v = Tile<T, DP>::four(t, row0 + j, b * 16 + 4 * g);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float v = Tile<T, DP>::at(t, row0 + j, b * 16 + 4 * g + r);
-          if (w != 0.f) acc[b][nb][r] += w * v;
-        }
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (w[nb] != 0.f) acc[b][nb][r] += w[nb] * v[r];
+      __builtin_amdgcn_sched_barrier(0);                                     // four values at a time: the registers are the accumulators'
     }
   }
 }
@@ -286,6 +303,7 @@ __device__ __forceinline__ void accumulate_pairs(f32x4 (&acc)[DP / 16][NB], cons
 template <typename T, int DP, int ROWS>
 __device__ __forceinline__ bool any_not_finite(const unsigned char* t, int row0, int lane) {
   unsigned bad = 0;
+  asm volatile("");                                                          // only where it is asked for, not ahead of the branch
 #pragma unroll
   for (int i = 0; i < ROWS * Tile<T, DP>::kChunks / 64; ++i) {
     const uint4 w = *reinterpret_cast<const uint4*>(t + row0 * Tile<T, DP>::kPitch + (i * 64 + lane) * 16);
@@ -299,10 +317,24 @@ __device__ __forceinline__ bool any_not_finite(const unsigned char* t, int row0,
   return __ballot(bad != 0) != 0;
 }
 
+// Scheduling hint for a run of N fragments, READS LDS reads each, every one used by USES products: AHEAD fragments are read before the first
+// product and one more behind each fragment's products.  Without it the compiler reads them all first, more than the registers hold.
+template <typename T, int N, int READS, int USES, int AHEAD>
+__device__ __forceinline__ void interleave_reads() {
+  if constexpr (sizeof(T) == 2) {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, USES, 0);
+      if (i + AHEAD < N) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    }
+  }
+}
+
 // Workgroup: NW wavefronts of 16 NB queries of one head; the keys pass by in tiles of 64, two tiles of K and V in LDS, the next
 // one on its way (direct-to-LDS) while one is worked on.
 template <typename T, int DP, int NB, int NW, bool BIAS>
-__global__ __launch_bounds__(NW * 64, 2) void k_attend(AttendArgs a, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
+__global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend(AttendArgs a, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
                                                        T* __restrict__ out, float* __restrict__ lse) {
   typedef Tile<T, DP> TL;
   typedef typename Frag<T>::type frag;
@@ -349,12 +381,15 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend(AttendArgs a, const T* __
     for (int b = 0; b < DB; ++b) acc[b][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const int lo = iw + off, top = lo + NB * 16 - 1;                          // positions of the wavefront's rows
-  for (int t = 0; t < tiles; ++t) {
+  // A tile; MASKED: some pair of the workgroup's may not be visible.  Two loops and not one with a branch: with both ways of adding up in
+  // one loop the compiler keeps two sets of accumulators.
+  auto step = [&](int t, auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
     wait_vmcnt<0>();
     __syncthreads();
     if (t + 1 < tiles) stage(t + 1);
     const int kb = t * kTileKeys;
-    if (iw >= sp.nq || (a.causal && kb > top)) continue;
+    if (iw >= sp.nq || (MASKED && a.causal && kb > top)) return;
     const unsigned char* K = smem + (t & 1) * 2 * TL::kBytes;
     const unsigned char* V = K + TL::kBytes;
     f32x4 s[MB][NB];
@@ -369,6 +404,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend(AttendArgs a, const T* __
         for (int nb = 0; nb < NB; ++nb) s[mb][nb] = mma(s[mb][nb], kf, qf[nb][ks]);
       }
     }
+    interleave_reads<T, MB * KS, 1, NB, 4>();
     float mul = a.c, add = 0.f;
     if (BIAS) {
       const int rmax = kb + kTileKeys - 1 - lo, rmin = kb - top;
@@ -386,8 +422,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend(AttendArgs a, const T* __
         }
       }
     }
-    const bool masked = kb + kTileKeys > sp.nk || (a.causal && kb + kTileKeys - 1 > lo);
-    if (masked) {
+    if (MASKED) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const int end = a.causal ? min(sp.nk, lo + nb * 16 + l16 + 1) : sp.nk;   // keys before it are visible
@@ -404,7 +439,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend(AttendArgs a, const T* __
     for (int nb = 0; nb < NB; ++nb) {
       mx[nb] = kNegInf;
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb) mx[nb] = fmaxf(mx[nb], fmaxf(fmaxf(s[mb][nb][0], s[mb][nb][1]), fmaxf(s[mb][nb][2], s[mb][nb][3])));
+      for (int mb = 0; mb < MB; ++mb) mx[nb] = larger(larger(larger(larger(mx[nb], s[mb][nb][0]), s[mb][nb][1]), s[mb][nb][2]), s[mb][nb][3]);
       mx[nb] = fmaf(row_max(mx[nb]), mul, add);
       grow |= mx[nb] > m[nb] + kMaxSlack;
     }
@@ -418,22 +453,20 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend(AttendArgs a, const T* __
         for (int b = 0; b < DB; ++b) acc[b][nb] *= f;
       }
     }
+    const bool slow = MASKED && any_not_finite<T, DP, kTileKeys>(V, 0, lane);
+    auto exps = [&](int h2) {
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const float sub = add - m[nb];
+      for (int nb = 0; nb < NB; ++nb) {
+        const float sub = add - m[nb];
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb)
+        for (int mb = 2 * h2; mb < 2 * h2 + 2; ++mb) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[mb][nb][r], mul, sub));
-          l[nb] += p;
-          s[mb][nb][r] = p;
+          for (int r = 0; r < 4; ++r) s[mb][nb][r] = __builtin_amdgcn_exp2f(fmaf(s[mb][nb][r], mul, sub));
+          l[nb] += (s[mb][nb][0] + s[mb][nb][1]) + (s[mb][nb][2] + s[mb][nb][3]);
         }
-    }
-    if (masked && any_not_finite<T, DP, kTileKeys>(V, 0, lane)) {
-      accumulate_pairs<T, DP, NB, MB>(acc, s, V, 0, lane);
-      continue;
-    }
+      }
+    };
+    exps(0);
 #pragma unroll
     for (int h2 = 0; h2 < MB / 2; ++h2) {
       frag pf[NB];
@@ -441,6 +474,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend(AttendArgs a, const T* __
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int j = 0; j < 8; ++j) pf[nb][j] = (T)s[h2 * 2 + (j >> 2)][nb][j & 3];
+      if (h2 == 0) exps(1);
+      if (MASKED && slow) {
+        accumulate_pairs<T, DP, NB>(acc, pf, V, h2 * 32, lane);
+        continue;
+      }
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
         const frag vf = TL::col_frag(V, b, h2, lane);
@@ -448,7 +486,12 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend(AttendArgs a, const T* __
         for (int nb = 0; nb < NB; ++nb) acc[b][nb] = mma(acc[b][nb], vf, pf[nb]);
       }
     }
-  }
+    if (!MASKED) interleave_reads<T, DB * MB / 2, 2, NB, 3>();
+  };
+  const int full = min(sp.nk, a.causal ? max(0, i0 + off + 1) : sp.nk) / kTileKeys;         // tiles all of whose pairs are visible
+  int t = 0;
+  for (; t < min(full, tiles); ++t) step(t, std::false_type{});
+  for (; t < tiles; ++t) step(t, std::true_type{});
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int i = iw + nb * 16 + l16;
@@ -463,46 +506,126 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend(AttendArgs a, const T* __
 }
 
 // The same for few query rows a key head (single tokens against a cache): the rows of a workgroup are 16 of the pairs (query, head of
-// the group), so that a key head's rows are read once for its whole group, and the keys are dealt out: to `splits` workgroups in
+// the group), so that a key head's rows are read once for its whole group, and the keys are dealt out: to workgroups in
 // stretches, inside one to its wavefronts tile by tile.  A wavefront streams its tiles of 32 keys through LDS of its own, without
-// a barrier; what the wavefronts have is joined in LDS, what the workgroups have by k_attend_join.  HBM-bound.
+// a barrier, the next K on its way while V is worked on and the reverse; what the wavefronts have is joined in LDS, what the workgroups have by k_attend_join.  HBM-bound.
 constexpr int kFewRows = 16, kFewKeys = 32;
 template <typename T, int DP>
 constexpr int few_waves() { return DP * (int)sizeof(T) > 256 ? 2 : 4; }
 template <typename T, int DP>
-constexpr int few_lds() { return few_waves<T, DP>() * 4 * kFewKeys * DP * (int)sizeof(T); }
+constexpr int few_lds() { return few_waves<T, DP>() * 2 * kFewKeys * DP * (int)sizeof(T); }
+
+// How the keys are dealt out: all row tiles' key counts together make `stretches` stretches of about equal length, a row tile having at least
+// one to itself (stretches = 0: exactly one).  A stretch then is a row tile and a part of its keys; the partial results lie in the order of the
+// stretches.
+struct Stretch {
+  Span sp;                   // tile: the row tile
+  int part, parts, keys;     // which part of the row tile's keys, of how many, of how many keys each
+  int first;                 // stretch of the row tile's first part
+};
+__device__ __forceinline__ int wave_total(int v) {
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) v += __shfl_xor(v, w);
+  return __builtin_amdgcn_readfirstlane(v);
+}
+// The stretch of index `at`, or (by_tile) the first one of row tile `at`; false if there are not as many.
+__device__ __forceinline__ bool find_stretch(const AttendArgs& a, int stretches, int at, bool by_tile, Stretch& st) {
+  const int lane = threadIdx.x & 63, group = a.heads / a.kv_heads;
+  long keys = 0;
+  int tiles = 0;
+  int q0 = 0, nq = 0, k0 = 0, nk = 0;
+  for (int s0 = 0; s0 < a.sequences; s0 += 64) {
+    q0 = nq = k0 = nk = 0;
+    if (s0 + lane < a.sequences) read_span(a, s0 + lane, q0, nq, k0, nk);
+    const int n = (nq * group + kFewRows - 1) / kFewRows;
+    tiles += wave_total(n);
+    keys += (long)wave_total(n * (nk >> 10)) << 10;                          // in 1024s and the rest: no 32-bit overflow
+    keys += wave_total(n * (nk & 1023));
+  }
+  const int spare = stretches - tiles;
+  const long even = spare > 0 ? (keys + spare - 1) / spare : (long)a.rows_k + 1;
+  st.keys = (int)min(max((even + kFewKeys - 1) / kFewKeys * kFewKeys, 4L * kFewKeys), 1L << 30);
+  int first = 0;
+  for (int s0 = 0; s0 < a.sequences; s0 += 64) {
+    if (a.sequences > 64) {
+      q0 = nq = k0 = nk = 0;
+      if (s0 + lane < a.sequences) read_span(a, s0 + lane, q0, nq, k0, nk);
+    }
+    const int n = (nq * group + kFewRows - 1) / kFewRows, parts = max(1, (nk + st.keys - 1) / st.keys);
+    int upto = n * parts, upto_tiles = n;
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) {
+      const int v = __shfl_up(upto, w), u = __shfl_up(upto_tiles, w);
+      if (lane >= w) {
+        upto += v;
+        upto_tiles += u;
+      }
+    }
+    const int total = __builtin_amdgcn_readlane(by_tile ? upto_tiles : upto, 63);
+    if (at < total) {
+      const int l = __builtin_ctzll(__ballot(at < (by_tile ? upto_tiles : upto)));
+      st.sp.q0 = __builtin_amdgcn_readlane(q0, l);
+      st.sp.nq = __builtin_amdgcn_readlane(nq, l);
+      st.sp.k0 = __builtin_amdgcn_readlane(k0, l);
+      st.sp.nk = __builtin_amdgcn_readlane(nk, l);
+      st.sp.tiles = __builtin_amdgcn_readlane(n, l);
+      st.parts = __builtin_amdgcn_readlane(parts, l);
+      const int before = __builtin_amdgcn_readlane(upto, l) - st.sp.tiles * st.parts;   // stretches of the sequences before, of these 64
+      if (by_tile) {
+        st.sp.tile = at - (__builtin_amdgcn_readlane(upto_tiles, l) - st.sp.tiles);
+        st.part = 0;
+      } else {
+        st.sp.tile = (at - before) / st.parts;
+        st.part = (at - before) % st.parts;
+      }
+      st.first = first + before + st.sp.tile * st.parts;
+      return true;
+    }
+    at -= total;
+    first += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
 
 template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__((few_waves<T, DP>() * 64)) void k_attend_few(AttendArgs a, int splits, const T* __restrict__ q, const T* __restrict__ k,
+__global__ __launch_bounds__((few_waves<T, DP>() * 64)) void k_attend_few(AttendArgs a, int stretches, const T* __restrict__ q, const T* __restrict__ k,
                                                                         const T* __restrict__ v, T* __restrict__ out, float* __restrict__ lse,
                                                                         float* __restrict__ part, float* __restrict__ part_ml) {
   typedef Tile<T, DP> TL;
   typedef typename Frag<T>::type frag;
-  constexpr int KS = DP / 32, DB = DP / 16, NW = few_waves<T, DP>(), kHalf = kFewKeys * TL::kPitch;
+  constexpr int KS = DP / 32, DB = DP / 16, NW = few_waves<T, DP>(), kHalf = kFewKeys * TL::kPitch, kLoads = kFewKeys * TL::kChunks / 64;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   __shared__ float ml[NW][2][kFewRows];
-  const int group = a.heads / a.kv_heads, id = blockIdx.x;
-  const int kvh = id % a.kv_heads, split = id / a.kv_heads % splits, idx = id / a.kv_heads / splits;
-  Span sp;
-  if (!find_span(a, idx, [group](int nq, int) { return (nq * group + kFewRows - 1) / kFewRows; }, sp)) return;
+  const int group = a.heads / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
+  Stretch where;
+  if (!find_stretch(a, stretches, blockIdx.x / a.kv_heads, false, where)) return;
+  const Span& sp = where.sp;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
   const int rows = sp.nq * group, off = sp.nk - sp.nq;
   const int row = min(sp.tile * kFewRows + l16, rows - 1);                   // past the end: the last one again, not written
   const int i = row / group, h = kvh * group + row % group, pos = i + off;
   const int first_pos = sp.tile * kFewRows / group + off, last_pos = min((sp.tile + 1) * kFewRows - 1, rows - 1) / group + off;
   const int kend = a.causal ? min(sp.nk, max(0, last_pos + 1)) : sp.nk;
-  const int per = ((kend + splits - 1) / splits + kFewKeys - 1) / kFewKeys * kFewKeys;
-  const int c0 = min(split * per, kend), c1 = min(c0 + per, kend);
+  const int c0 = min(where.part * where.keys, kend), c1 = min(c0 + where.keys, kend);
   const int tiles = (c1 - c0 + kFewKeys - 1) / kFewKeys;
   const T* kb_ = k + (long)sp.k0 * a.ld_k + kvh * a.d;
   const T* vb_ = v + (long)sp.k0 * a.ld_v + kvh * a.d;
-  unsigned char* mine = smem + wave * 4 * kHalf;
-  auto stage = [&](int t, int slot) {
+  unsigned char* mine = smem + wave * 2 * kHalf;
+  const unsigned char* K = mine;
+  const unsigned char* V = mine + kHalf;
+  // past the last tile there is nothing to load, but as many loads are issued (of zeros): the waits count them
+  auto stage_k = [&](int t) {
     const int kb = c0 + t * kFewKeys;
-    TL::template stage<kFewKeys, 64>(kb_ + (long)kb * a.ld_k, a.ld_k, c1 - kb, a.d, mine + slot * 2 * kHalf, lane);
-    TL::template stage<kFewKeys, 64>(vb_ + (long)kb * a.ld_v, a.ld_v, c1 - kb, a.d, mine + slot * 2 * kHalf + kHalf, lane);
+    TL::template stage<kFewKeys, 64>(kb_ + (long)kb * a.ld_k, a.ld_k, c1 - kb, a.d, mine, lane);
   };
-  if (wave < tiles) stage(wave, 0);
+  auto stage_v = [&](int t) {
+    const int kb = c0 + t * kFewKeys;
+    TL::template stage<kFewKeys, 64>(vb_ + (long)kb * a.ld_v, a.ld_v, c1 - kb, a.d, mine + kHalf, lane);
+  };
+  if (wave < tiles) {
+    stage_k(wave);
+    stage_v(wave);
+  }
   frag qf[KS];
   const T* qrow = q + (long)(sp.q0 + i) * a.ld_q + h * a.d;
 #pragma unroll
@@ -516,12 +639,9 @@ __global__ __launch_bounds__((few_waves<T, DP>() * 64)) void k_attend_few(Attend
 #pragma unroll
   for (int b = 0; b < DB; ++b) acc[b][0] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = kLowest, l = 0.f;
-  for (int t = wave, slot = 0; t < tiles; t += NW, slot ^= 1) {
-    __builtin_amdgcn_s_waitcnt((0 << 8) | (7 << 4));                         // vmcnt(0) lgkmcnt(0): this tile is here, the one before is read
+  for (int t = wave; t < tiles; t += NW) {
+    wait_vmcnt<kLoads>();                                                    // K is here, V may be on its way
     __builtin_amdgcn_sched_barrier(0);
-    if (t + NW < tiles) stage(t + NW, slot ^ 1);
-    const unsigned char* K = mine + slot * 2 * kHalf;
-    const unsigned char* V = K + kHalf;
     const int kb = c0 + t * kFewKeys;
     f32x4 s[2][1];
 #pragma unroll
@@ -530,6 +650,9 @@ __global__ __launch_bounds__((few_waves<T, DP>() * 64)) void k_attend_few(Attend
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) s[mb][0] = mma(s[mb][0], TL::row_frag(K, mb, ks, lane), qf[ks]);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);                                      // lgkmcnt(0): K is read, its place takes the next one
+    stage_k(t + NW);
     float mul = a.c, add = 0.f;
     if (BIAS) {
       if (kb + kFewKeys - 1 - first_pos <= -a.last) add = far_left;
@@ -554,7 +677,7 @@ __global__ __launch_bounds__((few_waves<T, DP>() * 64)) void k_attend_few(Attend
     }
     float mx = kNegInf;
 #pragma unroll
-    for (int mb = 0; mb < 2; ++mb) mx = fmaxf(mx, fmaxf(fmaxf(s[mb][0][0], s[mb][0][1]), fmaxf(s[mb][0][2], s[mb][0][3])));
+    for (int mb = 0; mb < 2; ++mb) mx = larger(larger(larger(larger(mx, s[mb][0][0]), s[mb][0][1]), s[mb][0][2]), s[mb][0][3]);
     mx = fmaf(row_max(mx), mul, add);
     if (__ballot(mx > m + kMaxSlack)) {
       const float next = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - next);
@@ -572,17 +695,22 @@ __global__ __launch_bounds__((few_waves<T, DP>() * 64)) void k_attend_few(Attend
         l += p;
         s[mb][0][r] = p;
       }
+    frag pf[1];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) pf[0][j] = (T)s[j >> 2][0][j & 3];
+    wait_vmcnt<kLoads>();                                                    // V is here, the next K may be on its way
+    __builtin_amdgcn_sched_barrier(0);
     if (masked && any_not_finite<T, DP, kFewKeys>(V, 0, lane)) {
-      accumulate_pairs<T, DP, 1, 2>(acc, s, V, 0, lane);
-      continue;
+      accumulate_pairs<T, DP, 1>(acc, pf, V, 0, lane);
+    } else {
+#pragma unroll
+      for (int b = 0; b < DB; ++b) acc[b][0] = mma(acc[b][0], TL::col_frag(V, b, 0, lane), pf[0]);
     }
-    frag pf;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) pf[j] = (T)s[j >> 2][0][j & 3];
-#pragma unroll
-    for (int b = 0; b < DB; ++b) acc[b][0] = mma(acc[b][0], TL::col_frag(V, b, 0, lane), pf);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    stage_v(t + NW);
   }
-  __builtin_amdgcn_s_waitcnt((0 << 8) | (7 << 4));
+  __builtin_amdgcn_s_waitcnt((0 << 8) | (7 << 4));                           // nothing may still be on its way into LDS
   // join the wavefronts: each leaves its sums [16][DP] where its tiles were
   l = row_sum(l);
   float* own = reinterpret_cast<float*>(mine);
@@ -603,12 +731,12 @@ __global__ __launch_bounds__((few_waves<T, DP>() * 64)) void k_attend_few(Attend
     for (int w = 0; w < NW; ++w) {
       const float f = __builtin_amdgcn_exp2f(ml[w][0][rr] - mm);
       sum += ml[w][1][rr] * f;
-      o += *reinterpret_cast<const f32x4*>(smem + w * 4 * kHalf + (rr * DP + (d4 ^ (rr & 7)) * 4) * 4) * f;
+      o += *reinterpret_cast<const f32x4*>(smem + w * 2 * kHalf + (rr * DP + (d4 ^ (rr & 7)) * 4) * 4) * f;
     }
     const int at = sp.tile * kFewRows + rr;
     if (at >= rows) continue;
-    if (splits > 1) {
-      const size_t item = ((size_t)idx * a.kv_heads + kvh) * splits + split;
+    if (where.parts > 1) {
+      const size_t item = (size_t)(where.first + where.part) * a.kv_heads + kvh;
       *reinterpret_cast<f32x4*>(part + (item * kFewRows + rr) * DP + d4 * 4) = o;
       if (d4 == 0) {
         part_ml[(item * kFewRows + rr) * 2] = mm;
@@ -622,24 +750,28 @@ __global__ __launch_bounds__((few_waves<T, DP>() * 64)) void k_attend_few(Attend
   }
 }
 
-// Joins the splits of k_attend_few, in their order.  A thread takes four columns of a row.
+// Joins the parts of k_attend_few's row tiles, in their order.  A thread takes four columns of a row.
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int splits, const float* __restrict__ part, const float* __restrict__ part_ml,
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int stretches, const float* __restrict__ part, const float* __restrict__ part_ml,
                                                      T* __restrict__ out, float* __restrict__ lse) {
-  const int group = a.heads / a.kv_heads, kvh = blockIdx.x % a.kv_heads, idx = blockIdx.x / a.kv_heads;
-  Span sp;
-  if (!find_span(a, idx, [group](int nq, int) { return (nq * group + kFewRows - 1) / kFewRows; }, sp)) return;
-  const size_t item = ((size_t)idx * a.kv_heads + kvh) * splits;
+  const int group = a.heads / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
+  Stretch where;
+  if (!find_stretch(a, stretches, blockIdx.x / a.kv_heads, true, where) || where.parts == 1) return;
+  const Span& sp = where.sp;
+  const size_t pitch = (size_t)a.kv_heads * kFewRows;                        // rows of partial results from one part to the next
   for (int e = threadIdx.x; e < kFewRows * DP / 4; e += 256) {
     const int rr = e / (DP / 4), d4 = e % (DP / 4), at = sp.tile * kFewRows + rr;
     if (at >= sp.nq * group || d4 * 4 >= a.d) continue;
+    const size_t row = ((size_t)where.first * a.kv_heads + kvh) * kFewRows + rr;
     float mm = kLowest, sum = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) mm = fmaxf(mm, part_ml[((item + s) * kFewRows + rr) * 2]);
-    for (int s = 0; s < splits; ++s) {
-      const float f = __builtin_amdgcn_exp2f(part_ml[((item + s) * kFewRows + rr) * 2] - mm);
-      sum += part_ml[((item + s) * kFewRows + rr) * 2 + 1] * f;
-      o += *reinterpret_cast<const f32x4*>(part + ((item + s) * kFewRows + rr) * DP + d4 * 4) * f;
+#pragma unroll 8
+    for (int s = 0; s < where.parts; ++s) mm = fmaxf(mm, part_ml[(row + s * pitch) * 2]);
+#pragma unroll 8
+    for (int s = 0; s < where.parts; ++s) {
+      const float f = __builtin_amdgcn_exp2f(part_ml[(row + s * pitch) * 2] - mm);
+      sum += part_ml[(row + s * pitch) * 2 + 1] * f;
+      o += *reinterpret_cast<const f32x4*>(part + (row + s * pitch) * DP + d4 * 4) * f;
     }
     const int qi = sp.q0 + at / group, hh = kvh * group + at % group;
     store4(out + (long)qi * a.ld_o + hh * a.d + d4 * 4, o * (sum == 0.f ? 0.f : 1.f / sum));
@@ -757,17 +889,19 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
     for (int b = 0; b < DB; ++b) acc[b][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const int lo = iw + off, top = lo + NB * 16 - 1;
-  for (int t = 0; t < tiles; ++t) {
+  auto step = [&](int t, auto masked) {                                      // as in k_attend
+    constexpr bool MASKED = decltype(masked)::value;
     wait_vmcnt<0>();
     __syncthreads();
     if (t + 1 < tiles) stage(t + 1);
     const int kb = t * kTileKeys;
-    if (iw >= sp.nq || (a.causal && kb > top)) continue;
+    if (iw >= sp.nq || (MASKED && a.causal && kb > top)) return;
     const unsigned char* K = smem + (t & 1) * 2 * TL::kBytes;
     const unsigned char* V = K + TL::kBytes;
-    const bool masked = kb + kTileKeys > sp.nk || (a.causal && kb + kTileKeys - 1 > lo);
     int side = 0;                                                            // -1, 1: all pairs in the last bucket of that side
     if (BIAS) side = kb + kTileKeys - 1 - lo <= -a.last ? -1 : (kb - top >= a.last ? 1 : 0);
+    const float far = side < 0 ? far_left : side > 0 ? far_right : 0.f;
+    const bool slow = MASKED && any_not_finite<T, DP, kTileKeys>(K, 0, lane);
 #pragma unroll
     for (int h2 = 0; h2 < 2; ++h2) {
       f32x4 s[2][NB], dp[2][NB];
@@ -788,28 +922,29 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
           for (int nb = 0; nb < NB; ++nb) dp[mb][nb] = mma(dp[mb][nb], vf, dof[nb][ks]);
         }
       }
+      interleave_reads<T, 4 * KS, 1, NB, 4>();
+      if (BIAS && !side) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const float* tb = table + kb + h2 * 32 + 4 * g - (lo + nb * 16 + l16) + a.last + kPad;
+#pragma unroll
+          for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[mb][nb][r] = fmaf(s[mb][nb][r], a.c, tb[mb * 16 + r]);
+        }
+      }
+      const float mul = BIAS && !side ? 1.f : a.c;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        float add = -lse2[nb];
-        const float* tb = table + kb + h2 * 32 + 4 * g - (lo + nb * 16 + l16) + a.last + kPad;
-        if (BIAS && side) add += side < 0 ? far_left : far_right;
+        const float sub = far - lse2[nb];
+        const int end = a.causal ? min(sp.nk, lo + nb * 16 + l16 + 1) : sp.nk;
 #pragma unroll
         for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            float x = add;
-            if (BIAS && !side) x += tb[mb * 16 + r];
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[mb][nb][r], a.c, x));
-            s[mb][nb][r] = p * (dp[mb][nb][r] - delta[nb]);
+            const float ds = __builtin_amdgcn_exp2f(fmaf(s[mb][nb][r], mul, sub)) * (dp[mb][nb][r] - delta[nb]);
+            s[mb][nb][r] = MASKED && kb + h2 * 32 + mb * 16 + 4 * g + r >= end ? 0.f : ds;
           }
-        if (masked) {
-          const int end = a.causal ? min(sp.nk, lo + nb * 16 + l16 + 1) : sp.nk;
-#pragma unroll
-          for (int mb = 0; mb < 2; ++mb)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (kb + h2 * 32 + mb * 16 + 4 * g + r >= end) s[mb][nb][r] = 0.f;
-        }
       }
       if (BIAS && want_dbias) {
         if (side) {
@@ -827,23 +962,28 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
           BiasGrad<NB>::diagonals(pairs, sums + kb + h2 * 32 - lo + a.last + kPad, lane);
         }
       }
-      if (masked && any_not_finite<T, DP, 32>(K, h2 * 32, lane)) {
-        accumulate_pairs<T, DP, NB, 2>(acc, s, K, h2 * 32, lane);
-        continue;
-      }
       frag df[NB];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int j = 0; j < 8; ++j) df[nb][j] = (T)s[j >> 2][nb][j & 3];
+      if (MASKED && slow) {
+        accumulate_pairs<T, DP, NB>(acc, df, K, h2 * 32, lane);
+        continue;
+      }
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
         const frag kf = TL::col_frag(K, b, h2, lane);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) acc[b][nb] = mma(acc[b][nb], kf, df[nb]);
       }
+      if (!MASKED) interleave_reads<T, DB, 2, NB, 3>();
     }
-  }
+  };
+  const int full = min(sp.nk, a.causal ? max(0, i0 + off + 1) : sp.nk) / kTileKeys;
+  int t = 0;
+  for (; t < min(full, tiles); ++t) step(t, std::false_type{});
+  for (; t < tiles; ++t) step(t, std::true_type{});
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int i = iw + nb * 16 + l16;
@@ -939,10 +1079,11 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(
     for (int b = 0; b < DB; ++b) ak[b][nb] = av[b][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   float far_left = 0.f, far_right = 0.f;
-  for (int it = 0; it < steps; ++it) {
+  auto step = [&](int it, int tile, auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
     wait_vmcnt<0>();
     __syncthreads();
-    if (BIAS && it % per == 0) {
+    if (BIAS && tile == 0) {
       const int h = kvh * group + it / per;
       fill_bias_table<T, NT>(a, h, table, tid);
       far_left = bias_value<T>(a, h, a.side - 1);
@@ -950,67 +1091,62 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(
       __syncthreads();
     }
     if (it + 1 < steps) stage(it + 1);
-    const int qb = (first + it % per) * kTileKeys, lo = qb + off, top = lo + kTileKeys - 1;   // positions of the tile's queries
-    if (jw >= sp.nk || (a.causal && jw > top)) continue;
+    const int qb = (first + tile) * kTileKeys, lo = qb + off, top = lo + kTileKeys - 1;   // positions of the tile's queries
+    if (jw >= sp.nk || (MASKED && a.causal && jw > top)) return;
     const unsigned char* Q = smem + (it & 1) * kStage;
     const unsigned char* dO = Q + TL::kBytes;
     const float* st = reinterpret_cast<const float*>(dO + TL::kBytes);
-    const bool masked = qb + kTileKeys > sp.nq || (a.causal && jtop > lo);
     int side = 0;
     if (BIAS) side = jtop - lo <= -a.last ? -1 : (jw - top >= a.last ? 1 : 0);
+    const float far = side < 0 ? far_left : side > 0 ? far_right : 0.f;
+    const bool slow = MASKED && (any_not_finite<T, DP, kTileKeys>(dO, 0, lane) || any_not_finite<T, DP, kTileKeys>(Q, 0, lane));
 #pragma unroll
     for (int h2 = 0; h2 < 2; ++h2) {
-      f32x4 s[2][NB], dp[2][NB];
+      frag pf[NB], df[NB];
 #pragma unroll
       for (int mb = 0; mb < 2; ++mb) {
+        f32x4 s[NB], dp[NB];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s[mb][nb] = dp[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int nb = 0; nb < NB; ++nb) s[nb] = dp[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           const frag qf = TL::row_frag(Q, h2 * 2 + mb, ks, lane);
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) s[mb][nb] = mma(s[mb][nb], qf, kf[nb][ks]);
+          for (int nb = 0; nb < NB; ++nb) s[nb] = mma(s[nb], qf, kf[nb][ks]);
         }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           const frag of = TL::row_frag(dO, h2 * 2 + mb, ks, lane);
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) dp[mb][nb] = mma(dp[mb][nb], of, vf[nb][ks]);
+          for (int nb = 0; nb < NB; ++nb) dp[nb] = mma(dp[nb], of, vf[nb][ks]);
         }
-      }
-      const float far = side < 0 ? far_left : far_right;
-#pragma unroll
-      for (int mb = 0; mb < 2; ++mb) {
         const int row = (h2 * 2 + mb) * 16 + 4 * g;
         const f32x4 e = *reinterpret_cast<const f32x4*>(st + row), dl = *reinterpret_cast<const f32x4*>(st + 64 + row);
+        if (BIAS && !side) {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          const float* tb = table + jw + nb * 16 + l16 - (lo + row) + a.last + kPad;
+          for (int nb = 0; nb < NB; ++nb) {
+            const float* tb = table + jw + nb * 16 + l16 - (lo + row) + a.last + kPad;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float x = -e[r];
-            if (BIAS) x += side ? far : tb[-r];
-            float p = __builtin_amdgcn_exp2f(fmaf(s[mb][nb][r], a.c, x));
-            float ds = p * (dp[mb][nb][r] - dl[r]);
-            if (masked && (qb + row + r >= sp.nq || (a.causal && jw + nb * 16 + l16 > lo + row + r))) p = ds = 0.f;
-            s[mb][nb][r] = p;
-            dp[mb][nb][r] = ds;
+            for (int r = 0; r < 4; ++r) s[nb][r] = fmaf(s[nb][r], a.c, tb[-r]);
           }
         }
+        const float mul = BIAS && !side ? 1.f : a.c;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float p = __builtin_amdgcn_exp2f(fmaf(s[nb][r], mul, far - e[r]));
+            float ds = p * (dp[nb][r] - dl[r]);
+            if (MASKED && (qb + row + r >= sp.nq || (a.causal && jw + nb * 16 + l16 > lo + row + r))) p = ds = 0.f;
+            pf[nb][mb * 4 + r] = (T)p;
+            df[nb][mb * 4 + r] = (T)ds;
+          }
       }
-      if (masked && (any_not_finite<T, DP, 32>(dO, h2 * 32, lane) || any_not_finite<T, DP, 32>(Q, h2 * 32, lane))) {
-        accumulate_pairs<T, DP, NB, 2>(av, s, dO, h2 * 32, lane);
-        accumulate_pairs<T, DP, NB, 2>(ak, dp, Q, h2 * 32, lane);
+      if (MASKED && slow) {
+        accumulate_pairs<T, DP, NB>(av, pf, dO, h2 * 32, lane);
+        accumulate_pairs<T, DP, NB>(ak, df, Q, h2 * 32, lane);
         continue;
       }
-      frag pf[NB], df[NB];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          pf[nb][j] = (T)s[j >> 2][nb][j & 3];
-          df[nb][j] = (T)dp[j >> 2][nb][j & 3];
-        }
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
         const frag of = TL::col_frag(dO, b, h2, lane), qf = TL::col_frag(Q, b, h2, lane);
@@ -1020,6 +1156,16 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(
           ak[b][nb] = mma(ak[b][nb], qf, df[nb]);
         }
       }
+    }
+  };
+  // of a head's tiles: those with queries before some of the workgroup's keys, those all of whose pairs are visible, a short last one
+  const int whole = sp.nq / kTileKeys - first;                               // tiles before the short one
+  const int diag = a.causal ? max(0, min(per, (j0 + ROWS - 1 - off + kTileKeys - 1) / kTileKeys - first)) : 0;
+  int it = 0;
+  for (int hh = 0; hh < (steps > 0 ? group : 0); ++hh) {
+    for (int tile = 0; tile < per;) {
+      while (tile < per && (tile < diag || tile >= whole)) step(it++, tile++, std::true_type{});
+      while (tile < whole) step(it++, tile++, std::false_type{});
     }
   }
 #pragma unroll

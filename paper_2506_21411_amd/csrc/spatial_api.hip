@@ -77,11 +77,26 @@ long tiles_bound(long total, long sequences, int rows) { return total / rows + s
 
 int padded_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
-// How a forward call goes about its rows: few (k_attend_few, the keys dealt to `splits` workgroups) or tiles of 64 nb rows.
+// Rows of a workgroup: 16 nb a wavefront, nw wavefronts.
+struct TileShape {
+  int nb, nw;
+  int rows() const { return 16 * nb * nw; }
+};
+// Tiles of 64 rows where larger ones would leave compute units without work (and for fp32, whose fragments fill the registers); of 256 for
+// long sequences whose rows see every key (heads of more than 32: a tile of keys is a load for each of 512 threads); otherwise of 128, since a causal
+// tile's work grows with its rows and short sequences fill large tiles badly (eight of 77 to 2048 rows, us, 128 / 256: 55 / 74).  16 heads, 8192 rows, TFLOP/s with tiles
+// of 64 / 128 / 256: heads of 64 714 / 799 / 839, heads of 128 836 / 1107 / 1152; causal, 32 heads of 128 832 / 1069 / 1046.
+TileShape tile_shape(dchag_dtype dt, int d, long rows, long sequences, long heads, bool causal) {
+  if (dt != DCHAG_BF16 || tiles_bound(rows, sequences, 128) * heads < compute_units()) return {1, 4};
+  if (causal || d <= 32 || rows < 1024 * sequences || tiles_bound(rows, sequences, 256) * heads < compute_units()) return {2, 4};
+  return {2, 8};
+}
+
+// How a forward call goes about its rows: few (k_attend_few) or tiles of 64 nb rows.
 struct ForwardPlan {
   bool few;
-  int splits, nb;
-  long items;                 // row tiles at most
+  int nb, nw;                 // 16 nb rows a wavefront, nw wavefronts a workgroup
+  long items, stretches;      // row tiles at most; few: parts that they are dealt to, 0: not split
   size_t part, part_ml, total;
 };
 ForwardPlan forward_plan(dchag_dtype dt, const AttendArgs& a) {
@@ -90,30 +105,28 @@ ForwardPlan forward_plan(dchag_dtype dt, const AttendArgs& a) {
   const int group = a.heads / a.kv_heads;
   const long rows = (long)a.rows_q * group, seqs = std::min<long>(a.sequences, a.rows_q);
   p.few = rows <= 32L * seqs;
-  p.splits = 1;
   p.total = 256;
   if (p.few) {
     p.items = rows / kFewRows + std::min<long>(a.sequences, rows);
-    const int cus = compute_units();
-    const long base = p.items * a.kv_heads;
-    const long per_seq = a.rows_k / std::max(1, a.sequences);
-    if (base > 0) p.splits = (int)std::max(1L, std::min({3L * cus / base, per_seq / 256, 64L}));
-    if (p.splits > 1) {
-      const size_t n = (size_t)base * p.splits * kFewRows;
-      p.part = 0;
+    const long fill = 4L * compute_units() / a.kv_heads;                     // twice the workgroups that the chip holds at once
+    const bool split = p.items > 0 && p.items * 2 < fill && a.rows_k / std::max(1, a.sequences) >= 1024;
+    p.stretches = split ? fill : 0;
+    if (split) {
+      const size_t n = (size_t)p.stretches * a.kv_heads * kFewRows;
       p.part_ml = align_up(n * padded_dim(a.d) * 4);
       p.total = p.part_ml + align_up(n * 8);
     }
     return p;
   }
-  p.nb = dt == DCHAG_BF16 && tiles_bound(a.rows_q, a.sequences, 128) * a.heads >= compute_units() ? 2 : 1;
-  p.items = tiles_bound(a.rows_q, a.sequences, p.nb * 64);
+  const TileShape t = tile_shape(dt, a.d, a.rows_q, a.sequences, a.heads, a.causal);
+  p.nb = t.nb;
+  p.nw = t.nw;
+  p.items = tiles_bound(a.rows_q, a.sequences, t.rows());
   return p;
 }
 
-template <typename T, int DP, int NB, bool BIAS>
+template <typename T, int DP, int NB, int NW, bool BIAS>
 int launch_attend(const AttendArgs& a, const ForwardPlan& p, const void* q, const void* k, const void* v, void* out, float* lse, hipStream_t st) {
-  constexpr int NW = 4;
   const int lds = 4 * Tile<T, DP>::kBytes + (BIAS ? bias_table_size(a.last) * 4 : 0);
   auto kern = k_attend<T, DP, NB, NW, BIAS>;
   if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
@@ -133,12 +146,12 @@ int launch_few(const AttendArgs& a, const ForwardPlan& p, const void* q, const v
   float* ml = reinterpret_cast<float*>(ws + p.part_ml);
   {
     StageTimer tm(DCHAG_STAGE_ATTEND, st);
-    kern<<<dim3((unsigned)(p.items * a.kv_heads * p.splits)), few_waves<T, DP>() * 64, lds, st>>>(
-        a, p.splits, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), lse, part, ml);
+    kern<<<dim3((unsigned)(std::max(p.items, p.stretches) * a.kv_heads)), few_waves<T, DP>() * 64, lds, st>>>(
+        a, (int)p.stretches, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), lse, part, ml);
   }
-  if (p.splits > 1) {
+  if (p.stretches) {
     StageTimer tm(DCHAG_STAGE_ATTEND_JOIN, st);
-    k_attend_join<T, DP><<<dim3((unsigned)(p.items * a.kv_heads)), 256, 0, st>>>(a, p.splits, part, ml, static_cast<T*>(out), lse);
+    k_attend_join<T, DP><<<dim3((unsigned)(p.items * a.kv_heads)), 256, 0, st>>>(a, (int)p.stretches, part, ml, static_cast<T*>(out), lse);
   }
   return launch_status();
 }
@@ -148,21 +161,33 @@ int attend_dim(const AttendArgs& a, const ForwardPlan& p, const void* q, const v
                hipStream_t st) {
   if (p.few) return a.bias ? launch_few<T, DP, true>(a, p, q, k, v, out, lse, ws, st) : launch_few<T, DP, false>(a, p, q, k, v, out, lse, ws, st);
   if constexpr (sizeof(T) == 2)
-    if (p.nb == 2) return a.bias ? launch_attend<T, DP, 2, true>(a, p, q, k, v, out, lse, st) : launch_attend<T, DP, 2, false>(a, p, q, k, v, out, lse, st);
-  return a.bias ? launch_attend<T, DP, 1, true>(a, p, q, k, v, out, lse, st) : launch_attend<T, DP, 1, false>(a, p, q, k, v, out, lse, st);
+    if (p.nb == 2) {
+      if constexpr (DP > 32)
+        if (p.nw == 8) return a.bias ? launch_attend<T, DP, 2, 8, true>(a, p, q, k, v, out, lse, st) : launch_attend<T, DP, 2, 8, false>(a, p, q, k, v, out, lse, st);
+      return a.bias ? launch_attend<T, DP, 2, 4, true>(a, p, q, k, v, out, lse, st) : launch_attend<T, DP, 2, 4, false>(a, p, q, k, v, out, lse, st);
+    }
+  return a.bias ? launch_attend<T, DP, 1, 4, true>(a, p, q, k, v, out, lse, st) : launch_attend<T, DP, 1, 4, false>(a, p, q, k, v, out, lse, st);
 }
 
 struct BackwardPlan {
-  int nb_q, nb_k;
+  TileShape q, k;
   long items_q, items_k;
   size_t stat, dbias, total;
 };
+// Query tiles as in the forward pass, but with the bias gradient's sums a wavefront of 32 rows of a head of 128 does not fit its registers (2048 rows,
+// 32 heads, us, tiles of 16 x 4 / 32 x 4 / 32 x 8 / 16 x 8 rows: - / 342 / 153 / 143).  Key tiles of heads of 128 have 16 keys a wavefront, as two
+// sums and two operands of 32 do not fit either (4096 rows, 16 heads, us: 16 x 4 296, 16 x 8 291, 32 x 4 755; causal with
+// grouped heads, 10374 rows: 745, 867, 2905).
 BackwardPlan backward_plan(dchag_dtype dt, const AttendArgs& a) {
   BackwardPlan p;
-  p.nb_q = dt == DCHAG_BF16 && tiles_bound(a.rows_q, a.sequences, 128) * a.heads >= compute_units() ? 2 : 1;
-  p.nb_k = dt == DCHAG_BF16 && tiles_bound(a.rows_k, a.sequences, 128) * a.kv_heads >= compute_units() ? 2 : 1;
-  p.items_q = tiles_bound(a.rows_q, a.sequences, p.nb_q * 64);
-  p.items_k = tiles_bound(a.rows_k, a.sequences, p.nb_k * 64);
+  p.q = tile_shape(dt, a.d, a.rows_q, a.sequences, a.heads, a.causal);
+  p.k = tile_shape(dt, a.d, a.rows_k, a.sequences, a.kv_heads, true);
+  if (a.d > 64) {
+    if (a.bias && p.q.nb == 2) p.q = {1, 8};
+    p.k = {1, 4};
+  }
+  p.items_q = tiles_bound(a.rows_q, a.sequences, p.q.rows());
+  p.items_k = tiles_bound(a.rows_k, a.sequences, p.k.rows());
   p.stat = 0;
   p.dbias = align_up((size_t)2 * a.heads * a.rows_q * 4);
   p.total = p.dbias + align_up((size_t)p.items_q * a.heads * a.buckets * 4) + 256;
@@ -175,9 +200,8 @@ struct BackwardPtrs {
   void *dq, *dk, *dv, *dbias;
 };
 
-template <typename T, int DP, int NB, bool BIAS>
+template <typename T, int DP, int NB, int NW, bool BIAS>
 int launch_dq(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
-  constexpr int NW = 4;
   const int table = (bias_table_size(a.last) + 3) & ~3;
   const int lds = 4 * Tile<T, DP>::kBytes + (BIAS ? table * 4 * (NW + 1) + NW * BiasGrad<NB>::kPairs * 4 : 0);
   auto kern = k_attend_dq<T, DP, NB, NW, BIAS>;
@@ -190,9 +214,8 @@ int launch_dq(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t,
         t.dbias != nullptr);
   return launch_status();
 }
-template <typename T, int DP, int NB, bool BIAS>
+template <typename T, int DP, int NB, int NW, bool BIAS>
 int launch_dkv(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
-  constexpr int NW = 4;
   const int lds = 2 * dkv_stage_bytes<T, DP>() + (BIAS ? bias_table_size(a.last) * 4 : 0);
   auto kern = k_attend_dkv<T, DP, NB, NW, BIAS>;
   if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
@@ -207,12 +230,18 @@ int launch_dkv(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t
 template <typename T, int DP, bool BIAS>
 int backward_bias(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
   int rc;
-  if constexpr (sizeof(T) == 2) {
-    rc = p.nb_q == 2 ? launch_dq<T, DP, 2, BIAS>(a, p, t, ws, st) : launch_dq<T, DP, 1, BIAS>(a, p, t, ws, st);
-    if (!rc) rc = p.nb_k == 2 ? launch_dkv<T, DP, 2, BIAS>(a, p, t, ws, st) : launch_dkv<T, DP, 1, BIAS>(a, p, t, ws, st);
+  if constexpr (sizeof(T) == 4) {
+    rc = launch_dq<T, DP, 1, 4, BIAS>(a, p, t, ws, st);
+    if (!rc) rc = launch_dkv<T, DP, 1, 4, BIAS>(a, p, t, ws, st);
   } else {
-    rc = launch_dq<T, DP, 1, BIAS>(a, p, t, ws, st);
-    if (!rc) rc = launch_dkv<T, DP, 1, BIAS>(a, p, t, ws, st);
+    if (p.q.nb == 1 && p.q.nw == 4) rc = launch_dq<T, DP, 1, 4, BIAS>(a, p, t, ws, st);
+    else if constexpr (DP == 128 && BIAS) rc = launch_dq<T, DP, 1, 8, BIAS>(a, p, t, ws, st);
+    else if constexpr (DP == 32) rc = launch_dq<T, DP, 2, 4, BIAS>(a, p, t, ws, st);
+    else rc = p.q.nw == 8 ? launch_dq<T, DP, 2, 8, BIAS>(a, p, t, ws, st) : launch_dq<T, DP, 2, 4, BIAS>(a, p, t, ws, st);
+    if (!rc) {
+      if constexpr (DP == 128) rc = launch_dkv<T, DP, 1, 4, BIAS>(a, p, t, ws, st);
+      else rc = p.k.nb == 2 ? launch_dkv<T, DP, 2, 4, BIAS>(a, p, t, ws, st) : launch_dkv<T, DP, 1, 4, BIAS>(a, p, t, ws, st);
+    }
   }
   if (rc || !BIAS || !t.dbias) return rc;
   StageTimer tm(DCHAG_STAGE_BWD_ATTEND_BIAS, st);
@@ -301,7 +330,7 @@ int dchag_attend(dchag_dtype dt, const dchag_attention* att, const void* q, cons
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(lse)) return DCHAG_ERR_ALIGN;
   const ForwardPlan p = forward_plan(dt, a);
   if (bad_workspace(workspace, workspace_bytes, p.total)) return DCHAG_ERR_WORKSPACE;
-  if ((p.few ? p.items * a.kv_heads * p.splits : p.items * a.heads) > 0x7fffffffL) return DCHAG_ERR_SHAPE;
+  if ((p.few ? std::max(p.items, p.stretches) * a.kv_heads : p.items * a.heads) > 0x7fffffffL) return DCHAG_ERR_SHAPE;
   if (p.items == 0) return DCHAG_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
