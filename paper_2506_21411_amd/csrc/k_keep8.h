@@ -27,8 +27,16 @@ __device__ __forceinline__ void decode8(uint2 w, float sc, float (&v)[8]) {
     v[4 * k + 3] = hi[1] * sc;
   }
 }
+// The same as bf16 numbers: one instruction for two, which takes the scale's exponent (0 stands for 2^-127).
+__device__ __forceinline__ bf16x8 decode8_bf16(uint2 w, unsigned byte) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 b2;
+  const float sc = __builtin_bit_cast(float, byte << 23);
+  const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, sc, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, sc, true);
+  const b2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, sc, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, sc, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+  const f32x4 a = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + 4));
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     v[j] = a[j];
@@ -36,7 +44,7 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   }
 }
 __device__ __forceinline__ void load8(const bf16* p, float (&v)[8]) {
-  const bf16x8 a = *reinterpret_cast<const bf16x8*>(p);
+  const bf16x8 a = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(p));
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = (float)a[j];
 }
@@ -51,161 +59,217 @@ __device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
   *reinterpret_cast<bf16x8*>(p) = o;
 }
 
-// HBM-bound.  Four threads share a block of 32 values, eight each: a wavefront reads 16 blocks one behind the other.
-template <typename T>
-__global__ __launch_bounds__(256) void k_pack8(long rows, int D, long ld, const T* __restrict__ x, unsigned char* __restrict__ codes,
-                                               unsigned char* __restrict__ scales) {
-  const int blocks = (D + 31) / 32;
-  const long id = (long)blockIdx.x * 256 + threadIdx.x;
-  const long row = (id >> 2) / blocks;
-  const int blk = (int)((id >> 2) - row * blocks), e = blk * 32 + (int)(id & 3) * 8;
-  const bool in = row < rows && e < D;
-  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (in) load8(x + row * ld + e, v);
-  float top = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float m = fabsf(v[j]);
-    if (m <= -kLowest) top = fmaxf(top, m);
-    else v[j] = __builtin_nanf("");
+// Both HBM-bound.  Four threads share a block of 32 values, eight each.  A thread packs kTurns of its eights, whose loads are all on their way
+// before the first is used and pass the caches by, as do the codes (neither is needed again soon); it unpacks one, into the caches
+// (2^29 bf16 values, us: packing 259 this way, 292 one at a time through the caches; unpacking 253, four at a time 262).  Rows
+// without gaps whose blocks are all whole are one long row to the kernels (the host passes them so), which saves the division.
+constexpr int kTurns = 4;
+struct Rows8 {
+  long rows, D, ld, blocks;            // blocks of a row
+  // Element offsets in x (ld) and in the codes (D) of thread chunk id, and the block's index; false past the end.
+  __device__ __forceinline__ bool at(long id, long& x, long& code, long& block) const {
+    block = id >> 2;
+    const long row = rows == 1 ? 0 : block / blocks, e = (block - row * blocks) * 32 + (id & 3) * 8;
+    x = row * ld + e;
+    code = row * D + e;
+    return row < rows && e < D;
   }
-  top = fmaxf(top, dpp_move<kDppSwapPairs>(top));
-  top = fmaxf(top, dpp_move<kDppSwapHalves>(top));
-  const unsigned bits = __builtin_bit_cast(unsigned, top);
-  const int byte = max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 0);
-  if (!in) return;
-  const float sc = unscale_of(byte);
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_pack8(Rows8 r, const T* __restrict__ x, unsigned char* __restrict__ codes, unsigned char* __restrict__ scales) {
+  const long first = (long)blockIdx.x * (256 * kTurns) + threadIdx.x;
+  long code[kTurns], block[kTurns];
+  bool in[kTurns];
+  float v[kTurns][8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] *= sc;
-  if (byte == 247)                                                           // 256 * 2^120 is no number of T
+  for (int u = 0; u < kTurns; ++u) {
+    long at;
+    in[u] = r.at(first + u * 256, at, code[u], block[u]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (fabsf(v[j]) > 240.f) v[j] = copysignf(240.f, v[j]);
-  int w0 = 0, w1 = 0;
-  w0 = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], w0, false);
-  w0 = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w0, true);
-  w1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], w1, false);
-  w1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], w1, true);
-  *reinterpret_cast<uint2*>(codes + row * D + e) = make_uint2(w0, w1);
-  if ((id & 3) == 0) scales[row * blocks + blk] = (unsigned char)byte;
+    for (int j = 0; j < 8; ++j) v[u][j] = 0.f;
+    if (in[u]) load8(x + at, v[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < kTurns; ++u) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float m = fabsf(v[u][j]);
+      if (m <= -kLowest) top = fmaxf(top, m);
+      else v[u][j] = __builtin_nanf("");
+    }
+    top = fmaxf(top, dpp_move<kDppSwapPairs>(top));
+    top = fmaxf(top, dpp_move<kDppSwapHalves>(top));
+    const unsigned bits = __builtin_bit_cast(unsigned, top);
+    const int byte = max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 0);
+    if (!in[u]) continue;
+    const float sc = unscale_of(byte);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[u][j] *= sc;
+    if (byte == 247)                                                         // 256 * 2^120 is no number of T
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (fabsf(v[u][j]) > 240.f) v[u][j] = copysignf(240.f, v[u][j]);
+    int w0 = 0, w1 = 0;
+    w0 = __builtin_amdgcn_cvt_pk_fp8_f32(v[u][0], v[u][1], w0, false);
+    w0 = __builtin_amdgcn_cvt_pk_fp8_f32(v[u][2], v[u][3], w0, true);
+    w1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[u][4], v[u][5], w1, false);
+    w1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[u][6], v[u][7], w1, true);
+    typedef __attribute__((ext_vector_type(2))) int i2;
+    __builtin_nontemporal_store(i2{w0, w1}, reinterpret_cast<i2*>(codes + code[u]));
+    if ((threadIdx.x & 3) == 0) scales[block[u]] = (unsigned char)byte;
+  }
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_unpack8(long rows, int D, long ld, const unsigned char* __restrict__ codes,
-                                                 const unsigned char* __restrict__ scales, T* __restrict__ x) {
-  const int blocks = (D + 31) / 32;
-  const long id = (long)blockIdx.x * 256 + threadIdx.x;
-  const long row = (id >> 2) / blocks;
-  const int blk = (int)((id >> 2) - row * blocks), e = blk * 32 + (int)(id & 3) * 8;
-  if (row >= rows || e >= D) return;
+__global__ __launch_bounds__(256) void k_unpack8(Rows8 r, const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales, T* __restrict__ x) {
+  long at, code, block;
+  if (!r.at((long)blockIdx.x * 256 + threadIdx.x, at, code, block)) return;
   float v[8];
-  decode8(*reinterpret_cast<const uint2*>(codes + row * D + e), scale_of(scales[row * blocks + blk]), v);
-  store8(x + row * ld + e, v);
+  decode8(*reinterpret_cast<const uint2*>(codes + code), scale_of(scales[block]), v);
+  store8(x + at, v);
 }
 
 // dW[o][i] = sum over rows of dy[row][o] x[row][i], db[o] = sum of dy[row][o], x held in 8 bits.  MFMA-bound for long inputs.
-// Workgroup: 128 x 128 of dW over one stretch of the rows, four wavefronts of 64 x 64; slices of 64 rows of both operands lie in LDS as they
-// lie in memory (both have the sum's index as their row) and are read transposed.  dy comes by direct-to-LDS loads; of x a
-// thread takes one block of 32 codes, which it turns into numbers of T once for all that read them: every e4m3 value times a power of
-// two is a bf16 number (below 2^-126 it is rounded).  Stretches beyond one leave partial sums that k_grad_join adds up in their order.
-template <typename T>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_weight_grad8(int rows, int d_out, int d_in, long ld, int stretch,
+// Workgroup: OS x IS of dW over one stretch of the rows, its wavefronts NO x NI parts of 16 WO x 16 WI; slices of 64 rows of
+// both operands lie in LDS as they lie in memory (both have the sum's index as their row) and are read transposed.  dy comes by
+// direct-to-LDS loads; of x a thread takes half a block of 32 codes or a whole one, which it turns into numbers of T once for all that read them: every
+// e4m3 value times a power of two is a bf16 number (below 2^-126 it is rounded).  Stretches beyond one leave partial sums that
+// k_grad_join adds up in their order.  An XCD takes neighbouring parts of dW and one stretch, so that its L2 serves most of both operands.
+template <typename T, int WO, int WI, int NO, int NI>
+struct GradTile {
+  static constexpr int kThreads = 64 * NO * NI, kOut = 16 * WO * NO, kIn = 16 * WI * NI;
+  static constexpr int kLds = 3 * Tile<T, kOut>::kBytes + 2 * Tile<T, kIn>::kBytes;
+};
+template <typename T, int WO, int WI, int NO, int NI>
+__global__ __launch_bounds__((64 * NO * NI), sizeof(T) == 2 ? 2 : 1) void k_weight_grad8(int rows, int d_out, int d_in, long ld, int stretch, int splits,
                                                           const T* __restrict__ dy, const unsigned char* __restrict__ codes,
                                                           const unsigned char* __restrict__ scales, T* __restrict__ dW, T* __restrict__ db,
                                                           float* __restrict__ part) {
-  typedef Tile<T, 128> TL;
+  typedef GradTile<T, WO, WI, NO, NI> GT;
+  constexpr int NT = GT::kThreads, OS = GT::kOut, IS = GT::kIn, CH = 64 * IS / 8 / NT;   // CH: chunks of 8 codes a thread takes
+  typedef Tile<T, OS> TO;
+  typedef Tile<T, IS> TI;
   typedef typename Frag<T>::type frag;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
-  const int ni = (d_in + 127) / 128, no = (d_out + 127) / 128;
-  const int it = blockIdx.x % ni, ot = blockIdx.x / ni % no, sp = blockIdx.x / ni / no;
-  const int o0 = ot * 128, i0 = it * 128, r0 = sp * stretch, r1 = min(rows, r0 + stretch);
-  const int wo = (wave >> 1) * 64, wi = (wave & 1) * 64, blocks = (d_in + 31) / 32;
+  const int ni = (d_in + IS - 1) / IS, no = (d_out + OS - 1) / OS;
+  const int total = ni * no * splits, per = (total + kXcds - 1) / kXcds, work = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
+  if ((int)blockIdx.x / kXcds >= per || work >= total) return;
+  const int it = work % ni, ot = work / ni % no, sp = work / ni / no;
+  const int o0 = ot * OS, i0 = it * IS, r0 = sp * stretch, r1 = min(rows, r0 + stretch);
+  const int wo = wave / NI * WO, wi = wave % NI * WI, blocks = (d_in + 31) / 32;         // wo, wi in blocks of 16
   const int tiles = (r1 - r0 + 63) / 64;
-  const int xrow = tid >> 2, xblk = tid & 3, xe = i0 + xblk * 32;            // this thread's block of a slice
-  uint2 cw[4];
-  unsigned sc = 0;
+  constexpr int kPerRow = IS / 8 / CH;                                       // threads a row of x; a thread's chunks lie kPerRow apart
+  const int xrow = tid / kPerRow, xc = tid % kPerRow;
+  uint2 cw[CH];
+  unsigned sc[CH];
   auto load_x = [&](int t) {
     const int r = r0 + t * 64 + xrow;
-    const bool in = r < r1 && xe < d_in;
-    sc = in ? scales[(size_t)r * blocks + xe / 32] : 0;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      cw[c] = in && xe + c * 8 < d_in ? *reinterpret_cast<const uint2*>(codes + (size_t)r * d_in + xe + c * 8) : make_uint2(0, 0);
+    for (int c = 0; c < CH; ++c) {
+      const int e = i0 + (xc + c * kPerRow) * 8;
+      const bool in = r < r1 && e < d_in;
+      cw[c] = in ? *reinterpret_cast<const uint2*>(codes + (size_t)r * d_in + e) : make_uint2(0, 0);
+      sc[c] = in ? scales[(size_t)r * blocks + e / 32] : 0;
+    }
   };
   auto put_x = [&](int t) {
-    unsigned char* to = smem + (t & 1) * 2 * TL::kBytes + TL::kBytes + xrow * TL::kPitch;
-    const float s = scale_of(sc);
+    unsigned char* to = smem + 3 * TO::kBytes + (t & 1) * TI::kBytes + xrow * TI::kPitch;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      float v[8];
-      decode8(cw[c], s, v);
+    for (int c = 0; c < CH; ++c) {
+      const int chunk = xc + c * kPerRow;
       if constexpr (sizeof(T) == 2) {
-        store8(reinterpret_cast<bf16*>(to + ((xblk * 4 + c) ^ TL::swz(xrow)) * 16), v);
+        *reinterpret_cast<bf16x8*>(to + (chunk ^ TI::swz(xrow)) * 16) = decode8_bf16(cw[c], sc[c]);
       } else {
-        *reinterpret_cast<f32x4*>(to + ((xblk * 8 + 2 * c) ^ TL::swz(xrow)) * 16) = f32x4{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4*>(to + ((xblk * 8 + 2 * c + 1) ^ TL::swz(xrow)) * 16) = f32x4{v[4], v[5], v[6], v[7]};
+        float v[8];
+        decode8(cw[c], scale_of(sc[c]), v);
+        *reinterpret_cast<f32x4*>(to + ((chunk * 2) ^ TI::swz(xrow)) * 16) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4*>(to + ((chunk * 2 + 1) ^ TI::swz(xrow)) * 16) = f32x4{v[4], v[5], v[6], v[7]};
       }
     }
   };
   auto stage_dy = [&](int t) {
-    TL::template stage<64, 256>(dy + (long)(r0 + t * 64) * ld + o0, ld, r1 - r0 - t * 64, min(128, d_out - o0), smem + (t & 1) * 2 * TL::kBytes, tid);
+    TO::template stage<64, NT>(dy + (long)(r0 + t * 64) * ld + o0, ld, r1 - r0 - t * 64, min(OS, d_out - o0), smem + t % 3 * TO::kBytes, tid);
   };
-  const bool sums = it == 0 && (wave & 1) == 0;                              // these wavefronts also add up dy
   frag ones;
 #pragma unroll
   for (int j = 0; j < 8; ++j) ones[j] = (T)1.f;
-  f32x4 acc[4][4], bs[4];
+  // dy's sums are dealt out to the wavefronts and workgroups that share its fragments: this wavefront adds up those from slot on, ni * NI apart
+  constexpr int MOST = WO / NI;                                              // with one workgroup to a row of them
+  const int slot = it * NI + wave % NI, apart = ni * NI;
+  f32x4 acc[WO][WI], bs[MOST];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    bs[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < MOST; ++i) bs[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int i = 0; i < WO; ++i)
+#pragma unroll
+    for (int j = 0; j < WI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // In the middle of slice t the codes of slice t + 1, which have had a slice's time to come, go into LDS, and slice t + 2's loads are issued
+  // (three places for dy, two for x).  (Loads a slice ahead and the codes' turn at a slice's end: us, 1536 x 1024 over 32768 rows 129.)
+  auto advance = [&](int t) {
+    wait_vmcnt<0>();
+    if (t + 1 < tiles) put_x(t + 1);
+    if (t + 2 < tiles) {
+      load_x(t + 2);
+      stage_dy(t + 2);
+    }
+  };
   if (tiles > 0) {
     load_x(0);
     stage_dy(0);
-    put_x(0);
-  }
-  for (int t = 0; t < tiles; ++t) {
     wait_vmcnt<0>();
-    __syncthreads();
-    if (t + 1 < tiles) {
-      stage_dy(t + 1);
-      load_x(t + 1);
+    put_x(0);
+    if (tiles > 1) {
+      load_x(1);
+      stage_dy(1);
     }
-    const unsigned char* A = smem + (t & 1) * 2 * TL::kBytes;
-    const unsigned char* X = A + TL::kBytes;
+  }
+  auto run = [&](auto sums) {                                                // sums: how many fragments of dy this wavefront adds up
+    for (int t = 0; t < tiles; ++t) {
+      __syncthreads();
+      const unsigned char* A = smem + t % 3 * TO::kBytes;
+      const unsigned char* X = smem + 3 * TO::kBytes + (t & 1) * TI::kBytes;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      frag xf[4];
+      for (int s = 0; s < 2; ++s) {
+        if (s == 1) advance(t);
+        frag xf[WI];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) xf[j] = TL::col_frag(X, wi / 16 + j, s, lane);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const frag af = TL::col_frag(A, wo / 16 + i, s, lane);
+        for (int j = 0; j < WI; ++j) xf[j] = TI::col_frag(X, wi + j, s, lane);
         // x as the rows of the block, dy as its columns: a lane holds four adjacent entries of a row of dW
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = mma(acc[i][j], xf[j], af);
-        if (sums) bs[i] = mma(bs[i], ones, af);
+        for (int i = 0; i < WO; ++i) {
+          const frag af = TO::col_frag(A, wo + i, s, lane);
+#pragma unroll
+          for (int j = 0; j < WI; ++j) acc[i][j] = mma(acc[i][j], xf[j], af);
+        }
+#pragma unroll
+        for (int i = 0; i < decltype(sums)::value; ++i) bs[i] = mma(bs[i], ones, TO::col_frag(A, wo + slot + i * apart, s, lane));
       }
     }
-    if (t + 1 < tiles) put_x(t + 1);
+  };
+  const int mine = db && slot < WO ? (WO - 1 - slot) / apart + 1 : 0;
+  if (mine == 0) run(std::integral_constant<int, 0>{});
+  else if (MOST == 1 || mine == 1) run(std::integral_constant<int, 1>{});
+  else run(std::integral_constant<int, MOST>{});
+#pragma unroll
+  for (int i = 0; i < MOST; ++i) {
+    const int o = o0 + (wo + slot + i * apart) * 16 + l16;
+    if (i >= mine || g != 0 || o >= d_out) continue;
+    if (part) part[(size_t)splits * d_out * d_in + (size_t)sp * d_out + o] = bs[i][0];
+    else db[o] = from_f32<T>(bs[i][0]);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int o = o0 + wo + i * 16 + l16;
+  for (int i = 0; i < WO; ++i) {
+    const int o = o0 + (wo + i) * 16 + l16;
     if (o >= d_out) continue;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int c = i0 + wi + j * 16 + 4 * g;
+    for (int j = 0; j < WI; ++j) {
+      const int c = i0 + (wi + j) * 16 + 4 * g;
       if (c >= d_in) continue;
       if (part) *reinterpret_cast<f32x4*>(part + ((size_t)sp * d_out + o) * d_in + c) = acc[i][j];
       else store4(dW + (size_t)o * d_in + c, acc[i][j]);
-    }
-    if (sums && g == 0 && db) {
-      if (part) part[(size_t)gridDim.x / ni / no * d_out * d_in + (size_t)sp * d_out + o] = bs[i][0];
-      else db[o] = from_f32<T>(bs[i][0]);
     }
   }
 }

@@ -260,14 +260,19 @@ bool bad_workspace(const void* ws, size_t have, size_t need) {
 
 // ---- weight gradient from 8 bits ------------------------------------------------------------------------------------------
 struct GradPlan {
-  int tiles, splits, stretch;
+  int side, tiles, splits, stretch;
   size_t total;
 };
-GradPlan grad_plan(long rows, int d_out, int d_in) {
+// Squares of dW of 256 (bf16; a compute unit holds one), 128 (two) or 64, the largest that give every compute unit one, over as many stretches
+// of the rows as the chip holds.  1536 x 1024 over 32768 rows, us: squares of 128 156, of 256 123.
+GradPlan grad_plan(dchag_dtype dt, long rows, int d_out, int d_in) {
   GradPlan p;
-  p.tiles = ((d_out + 127) / 128) * ((d_in + 127) / 128);
-  const long most = (rows + 255) / 256;                                      // a stretch of fewer rows costs more in partial sums than it gains
-  p.splits = (int)std::max(1L, std::min({2L * compute_units() / p.tiles, most, 64L}));
+  const int cus = compute_units();
+  const long most = std::max(1L, (rows + 255) / 256);                        // a stretch of fewer rows costs more in partial sums than it gains
+  const auto count = [&](int side) { return (long)((d_out + side - 1) / side) * ((d_in + side - 1) / side); };
+  p.side = dt == DCHAG_BF16 && count(256) * most >= cus ? 256 : count(128) * most >= cus ? 128 : 64;
+  p.tiles = (int)count(p.side);
+  p.splits = (int)std::max(1L, std::min({(p.side == 256 ? 1L : 2L) * cus / p.tiles, most, 64L}));
   p.stretch = (int)(((rows + p.splits - 1) / p.splits + 63) / 64 * 64);
   if (p.stretch < 64) p.stretch = 64;
   p.splits = (int)std::max(1L, (rows + p.stretch - 1) / p.stretch);
@@ -280,25 +285,31 @@ int check_rows8(dchag_dtype dt, int64_t rows, int D, int64_t ld) {
   if (rows > (int64_t)0x7fffffff * 64 / ((D + 31) / 32)) return DCHAG_ERR_SHAPE;   // workgroups of 64 blocks
   return DCHAG_OK;
 }
+Rows8 rows8(int64_t rows, int D, int64_t ld) {
+  if (D % 32 == 0 && (ld == 0 || ld == D)) return Rows8{1, (long)rows * D, (long)rows * D, (long)rows * (D / 32)};
+  return Rows8{(long)rows, D, ld ? (long)ld : D, (D + 31) / 32};
+}
+unsigned rows8_grid(const Rows8& r, int turns) { return (unsigned)((r.rows * r.blocks * 4 + 256 * turns - 1) / (256 * turns)); }
 int check_grad8(dchag_dtype dt, int rows, int d_out, int d_in, int64_t ld) {
   if (dt != DCHAG_F32 && dt != DCHAG_BF16) return DCHAG_ERR_DTYPE;
   if (rows < 0 || d_out < 8 || d_in < 8 || d_out % 8 || d_in % 8 || d_out > (1 << 20) || d_in > (1 << 20)) return DCHAG_ERR_SHAPE;
   if (ld != 0 && (ld < d_out || ld % 8 || ld > (1 << 23))) return DCHAG_ERR_SHAPE;
-  if ((int64_t)((d_out + 127) / 128) * ((d_in + 127) / 128) > (1 << 20)) return DCHAG_ERR_SHAPE;
+  if ((int64_t)((d_out + 63) / 64) * ((d_in + 63) / 64) > (1 << 22)) return DCHAG_ERR_SHAPE;
   return DCHAG_OK;
 }
 
-template <typename T>
+template <typename T, int WO, int WI, int NO, int NI>
 int launch_grad8(const GradPlan& p, int rows, int d_out, int d_in, long ld, const void* dy, const void* codes, const void* scales, void* dW, void* db,
                  float* part, hipStream_t st) {
-  auto kern = k_weight_grad8<T>;
-  constexpr int lds = 4 * Tile<T, 128>::kBytes;
+  typedef GradTile<T, WO, WI, NO, NI> GT;
+  auto kern = k_weight_grad8<T, WO, WI, NO, NI>;
+  constexpr int lds = GT::kLds;
   if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
   {
     StageTimer tm(DCHAG_STAGE_WEIGHT_GRAD8, st);
-    kern<<<dim3((unsigned)(p.tiles * p.splits)), 256, lds, st>>>(rows, d_out, d_in, ld, p.stretch, static_cast<const T*>(dy),
-                                                               static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales),
-                                                               static_cast<T*>(dW), static_cast<T*>(db), p.splits > 1 ? part : nullptr);
+    kern<<<dim3((unsigned)((p.tiles * p.splits + kXcds - 1) / kXcds * kXcds)), GT::kThreads, lds, st>>>(
+        rows, d_out, d_in, ld, p.stretch, p.splits, static_cast<const T*>(dy), static_cast<const unsigned char*>(codes),
+        static_cast<const unsigned char*>(scales), static_cast<T*>(dW), static_cast<T*>(db), p.splits > 1 ? part : nullptr);
   }
   if (p.splits > 1) {
     StageTimer tm(DCHAG_STAGE_WEIGHT_GRAD8, st);
@@ -374,13 +385,12 @@ int dchag_pack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void* x, 
   if (!x || !codes || !scales) return DCHAG_ERR_NULL;
   if (misaligned(x) || misaligned(codes) || misaligned(scales)) return DCHAG_ERR_ALIGN;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const long groups = (rows * ((D + 31) / 32) + 63) / 64;
+  const Rows8 r = rows8(rows, D, ld);
+  unsigned char *c = static_cast<unsigned char*>(codes), *e = static_cast<unsigned char*>(scales);
   set_level(0);
   StageTimer tm(DCHAG_STAGE_PACK8, st);
-  if (dt == DCHAG_F32)
-    k_pack8<float><<<dim3((unsigned)groups), 256, 0, st>>>(rows, D, ld ? ld : D, static_cast<const float*>(x), static_cast<unsigned char*>(codes), static_cast<unsigned char*>(scales));
-  else
-    k_pack8<bf16><<<dim3((unsigned)groups), 256, 0, st>>>(rows, D, ld ? ld : D, static_cast<const bf16*>(x), static_cast<unsigned char*>(codes), static_cast<unsigned char*>(scales));
+  if (dt == DCHAG_F32) k_pack8<float><<<rows8_grid(r, kTurns), 256, 0, st>>>(r, static_cast<const float*>(x), c, e);
+  else k_pack8<bf16><<<rows8_grid(r, kTurns), 256, 0, st>>>(r, static_cast<const bf16*>(x), c, e);
   return launch_status();
 }
 
@@ -391,19 +401,18 @@ int dchag_unpack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void* c
   if (!x || !codes || !scales) return DCHAG_ERR_NULL;
   if (misaligned(x) || misaligned(codes) || misaligned(scales)) return DCHAG_ERR_ALIGN;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const long groups = (rows * ((D + 31) / 32) + 63) / 64;
+  const Rows8 r = rows8(rows, D, ld);
+  const unsigned char *c = static_cast<const unsigned char*>(codes), *e = static_cast<const unsigned char*>(scales);
   set_level(0);
   StageTimer tm(DCHAG_STAGE_UNPACK8, st);
-  if (dt == DCHAG_F32)
-    k_unpack8<float><<<dim3((unsigned)groups), 256, 0, st>>>(rows, D, ld ? ld : D, static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales), static_cast<float*>(x));
-  else
-    k_unpack8<bf16><<<dim3((unsigned)groups), 256, 0, st>>>(rows, D, ld ? ld : D, static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales), static_cast<bf16*>(x));
+  if (dt == DCHAG_F32) k_unpack8<float><<<rows8_grid(r, 1), 256, 0, st>>>(r, c, e, static_cast<float*>(x));
+  else k_unpack8<bf16><<<rows8_grid(r, 1), 256, 0, st>>>(r, c, e, static_cast<bf16*>(x));
   return launch_status();
 }
 
 size_t dchag_weight_grad8_workspace_bytes(dchag_dtype dt, int rows, int d_out, int d_in) {
   if (check_grad8(dt, rows, d_out, d_in, 0)) return 0;
-  return grad_plan(rows, d_out, d_in).total;
+  return grad_plan(dt, rows, d_out, d_in).total;
 }
 
 int dchag_weight_grad8(dchag_dtype dt, int rows, int d_out, int d_in, int64_t ld, const void* dy, const void* codes, const void* scales, void* dW,
@@ -412,13 +421,15 @@ int dchag_weight_grad8(dchag_dtype dt, int rows, int d_out, int d_in, int64_t ld
   if (rc) return rc;
   if (!dW || (rows > 0 && (!dy || !codes || !scales))) return DCHAG_ERR_NULL;
   if (misaligned(dy) || misaligned(codes) || misaligned(scales) || misaligned(dW) || misaligned(db)) return DCHAG_ERR_ALIGN;
-  const GradPlan p = grad_plan(rows, d_out, d_in);
+  const GradPlan p = grad_plan(dt, rows, d_out, d_in);
   if (bad_workspace(workspace, workspace_bytes, p.total)) return DCHAG_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   set_level(0);
   float* part = static_cast<float*>(workspace);
-  if (dt == DCHAG_F32) return launch_grad8<float>(p, rows, d_out, d_in, ld ? ld : d_out, dy, codes, scales, dW, db, part, st);
-  return launch_grad8<bf16>(p, rows, d_out, d_in, ld ? ld : d_out, dy, codes, scales, dW, db, part, st);
+  const auto launch = dt == DCHAG_F32 ? (p.side == 64 ? launch_grad8<float, 2, 2, 2, 2> : launch_grad8<float, 4, 4, 2, 2>)
+                      : p.side == 64  ? launch_grad8<bf16, 2, 2, 2, 2>
+                      : p.side == 128 ? launch_grad8<bf16, 4, 4, 2, 2> : launch_grad8<bf16, 8, 4, 2, 4>;
+  return launch(p, rows, d_out, d_in, ld ? ld : d_out, dy, codes, scales, dW, db, part, st);
 }
 
 }  // extern "C"

@@ -83,7 +83,8 @@ def weight_grad(dtype, rows, d_in, d_out, seed=3):
     return dy, codes, held, (dW, n * (g.abs().T @ x.abs()) + u * dW.abs()), (db, n * g.abs().sum(0) + u * db.abs())
 
 
-SIZES = [(1, 8, 8), (5, 40, 24), (64, 128, 128), (300, 136, 264), (1000, 1000, 72), (2100, 264, 136), (0, 16, 24)]
+# the last sizes take squares of 128 and of 256 of dW on a device of up to 256 compute units
+SIZES = [(1, 8, 8), (5, 40, 24), (64, 128, 128), (300, 136, 264), (1000, 1000, 72), (2100, 264, 136), (0, 16, 24), (6000, 392, 1000), (9000, 1032, 648)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -104,6 +105,25 @@ def test_weight_gradient_of_a_part_of_the_columns():
     got = dchag.dchag_weight_grad8(room[:, 16:80], codes.cuda(), held.cuda())
     ref.check("dW", got[0], *dW)
     ref.check("db", got[1], *db)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_weight_gradient_reads_every_code(dtype):
+    """One row of dy picks one row of x: all codes at many exponents, the smallest and the largest among them, come out as they stand."""
+    codes = torch.arange(256, dtype=torch.uint8).repeat(64, 1)
+    codes[codes & 127 == 127] = 0                                  # NaN
+    held = torch.randint(30, 220, (64, 8), generator=torch.Generator().manual_seed(7)).to(torch.uint8)
+    held[0], held[1], held[2] = 0, 1, 246
+    want = dchag.dchag_unpack8(codes.cuda(), held.cuda(), torch.float32).cpu()
+    byte = held.long().repeat_interleave(32, 1).double()
+    c = codes.long()
+    mag = torch.where(c & 127 < 8, (c & 7) / 8.0 * 2.0 ** -6, (1 + (c & 7) / 8.0) * torch.exp2(((c >> 3) & 15).double() - 7))
+    value = torch.where(c > 127, -mag, mag) * torch.exp2(byte - 127)
+    assert torch.equal(want.double(), value)
+    dW, db = dchag.dchag_weight_grad8(torch.eye(64).to(TDT[dtype]).cuda(), codes.cuda(), held.cuda())
+    tiny = torch.finfo(torch.float32).smallest_normal               # products below the normal numbers may come out as zero
+    ok = (dW.double().cpu() == value.to(TDT[dtype]).double()) | (value.abs() < tiny)
+    assert bool(ok.all()) and bool((db == 1).all())
 
 
 def test_values_past_32_bits():
