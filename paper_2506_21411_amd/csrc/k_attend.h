@@ -881,14 +881,89 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
     delta[nb] = row_sum(dot);
     const float e = lse[(size_t)hi.h * a.rows_q + row];
     lse2[nb] = in && e != kNegInf ? e * kLog2e : __builtin_inff();          // a row that sees no key: P = 0
-    if (g == 0 && in) {
-      stat[(size_t)hi.h * a.rows_q + row] = lse2[nb];
-      stat[(size_t)(a.heads + hi.h) * a.rows_q + row] = delta[nb];
-    }
 #pragma unroll
     for (int b = 0; b < DB; ++b) acc[b][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const int lo = iw + off, top = lo + NB * 16 - 1;
+  // P (into s) and dP of 32 keys of tile t, the second half of it if h2; P of a pair that is not visible is 0, and so is its dP.
+  auto pairs_of = [&](int t, int h2, auto masked, f32x4 (&s)[2][NB], f32x4 (&dp)[2][NB], int side) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const unsigned char* K = smem + (t & 1) * 2 * TL::kBytes;
+    const unsigned char* V = K + TL::kBytes;
+    const int kb = t * kTileKeys;
+#pragma unroll
+    for (int mb = 0; mb < 2; ++mb) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) s[mb][nb] = dp[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const frag kf = TL::row_frag(K, h2 * 2 + mb, ks, lane);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) s[mb][nb] = mma(s[mb][nb], kf, qf[nb][ks]);
+      }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const frag vf = TL::row_frag(V, h2 * 2 + mb, ks, lane);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) dp[mb][nb] = mma(dp[mb][nb], vf, dof[nb][ks]);
+      }
+    }
+    interleave_reads<T, 4 * KS, 1, NB, 4>();
+    if (BIAS && !side) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const float* tb = table + kb + h2 * 32 + 4 * g - (lo + nb * 16 + l16) + a.last + kPad;
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[mb][nb][r] = fmaf(s[mb][nb][r], a.c, tb[mb * 16 + r]);
+      }
+    }
+    const float mul = BIAS && !side ? 1.f : a.c, far = side < 0 ? far_left : side > 0 ? far_right : 0.f;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float sub = far - lse2[nb];
+      const int end = a.causal ? min(sp.nk, lo + nb * 16 + l16 + 1) : sp.nk;
+#pragma unroll
+      for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[mb][nb][r] = __builtin_amdgcn_exp2f(fmaf(s[mb][nb][r], mul, sub));
+          if (MASKED && kb + h2 * 32 + mb * 16 + 4 * g + r >= end) s[mb][nb][r] = dp[mb][nb][r] = 0.f;
+        }
+    }
+  };
+  // -1, 1: all pairs of the tile are in the last bucket of that side
+  auto side_of = [&](int kb) { return !BIAS ? 0 : kb + kTileKeys - 1 - lo <= -a.last ? -1 : kb - top >= a.last ? 1 : 0; };
+  // delta from out as it was rounded to bf16 is off by up to 2^-8 <|do|, |out|>, which counts where few keys share a row's weight (dq's and dk's
+  // error against 64 bits, 16 to 100 keys: 1.85 times that of the two roundings of P and dS alone).  So where a row has at most two tiles of
+  // keys, which then both lie in LDS, it is added up from the pairs first: sum of P dP.
+  if (sizeof(T) == 2 && tiles <= 2) {
+    if (tiles == 2) stage(1);
+    wait_vmcnt<0>();
+    __syncthreads();
+    float sum[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) sum[nb] = 0.f;
+#pragma unroll 1
+    for (int u = 0; u < 2 * tiles; ++u) {
+      f32x4 s[2][NB], dp[2][NB];
+      pairs_of(u >> 1, u & 1, std::true_type{}, s, dp, side_of((u >> 1) * kTileKeys));
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sum[nb] = fmaf(s[mb][nb][r], dp[mb][nb][r], sum[nb]);
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) delta[nb] = row_sum(sum[nb]);
+  }
+  // Bias gradient: rows' sums of dS, which delta's error alone makes differ from 0, and of P in the last bucket of each side; the error's share
+  // of the last buckets is taken out at the end (2048 rows, 32 heads of 128: dbias' error against 64 bits 0.0031 -> 0.0016).
+  float rest[NB], far_p[NB][2];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) rest[nb] = far_p[nb][0] = far_p[nb][1] = 0.f;
   auto step = [&](int t, auto masked) {                                      // as in k_attend
     constexpr bool MASKED = decltype(masked)::value;
     wait_vmcnt<0>();
@@ -897,64 +972,41 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
     const int kb = t * kTileKeys;
     if (iw >= sp.nq || (MASKED && a.causal && kb > top)) return;
     const unsigned char* K = smem + (t & 1) * 2 * TL::kBytes;
-    const unsigned char* V = K + TL::kBytes;
-    int side = 0;                                                            // -1, 1: all pairs in the last bucket of that side
-    if (BIAS) side = kb + kTileKeys - 1 - lo <= -a.last ? -1 : (kb - top >= a.last ? 1 : 0);
-    const float far = side < 0 ? far_left : side > 0 ? far_right : 0.f;
+    const int side = side_of(kb);
     const bool slow = MASKED && any_not_finite<T, DP, kTileKeys>(K, 0, lane);
 #pragma unroll
     for (int h2 = 0; h2 < 2; ++h2) {
       f32x4 s[2][NB], dp[2][NB];
-#pragma unroll
-      for (int mb = 0; mb < 2; ++mb) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s[mb][nb] = dp[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const frag kf = TL::row_frag(K, h2 * 2 + mb, ks, lane);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) s[mb][nb] = mma(s[mb][nb], kf, qf[nb][ks]);
-        }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const frag vf = TL::row_frag(V, h2 * 2 + mb, ks, lane);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) dp[mb][nb] = mma(dp[mb][nb], vf, dof[nb][ks]);
-        }
-      }
-      interleave_reads<T, 4 * KS, 1, NB, 4>();
-      if (BIAS && !side) {
+      pairs_of(t, h2, masked, s, dp, side);
+      if (BIAS && want_dbias && side) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const float* tb = table + kb + h2 * 32 + 4 * g - (lo + nb * 16 + l16) + a.last + kPad;
+          float sum = 0.f;
 #pragma unroll
-          for (int mb = 0; mb < 2; ++mb)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) s[mb][nb][r] = fmaf(s[mb][nb][r], a.c, tb[mb * 16 + r]);
+          for (int mb = 0; mb < 2; ++mb) sum += (s[mb][nb][0] + s[mb][nb][1]) + (s[mb][nb][2] + s[mb][nb][3]);
+          if (side < 0) far_p[nb][0] += sum;
+          else far_p[nb][1] += sum;
         }
       }
-      const float mul = BIAS && !side ? 1.f : a.c;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const float sub = far - lse2[nb];
-        const int end = a.causal ? min(sp.nk, lo + nb * 16 + l16 + 1) : sp.nk;
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float ds = __builtin_amdgcn_exp2f(fmaf(s[mb][nb][r], mul, sub)) * (dp[mb][nb][r] - delta[nb]);
-            s[mb][nb][r] = MASKED && kb + h2 * 32 + mb * 16 + 4 * g + r >= end ? 0.f : ds;
-          }
-      }
+          for (int r = 0; r < 4; ++r) s[mb][nb][r] *= dp[mb][nb][r] - delta[nb];
       if (BIAS && want_dbias) {
-        if (side) {
+        float all = 0.f;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
           float sum = 0.f;
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int mb = 0; mb < 2; ++mb) sum += (s[mb][nb][0] + s[mb][nb][1]) + (s[mb][nb][2] + s[mb][nb][3]);
-          if (side < 0) sum_left += sum;
-          else sum_right += sum;
+          for (int mb = 0; mb < 2; ++mb) sum += (s[mb][nb][0] + s[mb][nb][1]) + (s[mb][nb][2] + s[mb][nb][3]);
+          rest[nb] += sum;
+          all += sum;
+        }
+        if (side) {
+          if (side < 0) sum_left += all;
+          else sum_right += all;
         } else {
           asm volatile("" ::: "memory");                                     // lanes read what other lanes of the wavefront wrote: in program order
           BiasGrad<NB>::put(pairs, s, lane);
@@ -984,6 +1036,20 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
   int t = 0;
   for (; t < min(full, tiles); ++t) step(t, std::false_type{});
   for (; t < tiles; ++t) step(t, std::true_type{});
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int i = iw + nb * 16 + l16;
+    if (BIAS && want_dbias) {
+      const float off_by = row_sum(rest[nb]);
+      sum_left -= off_by * far_p[nb][0];
+      sum_right -= off_by * far_p[nb][1];
+      delta[nb] += off_by;
+    }
+    if (g == 0 && i < sp.nq) {
+      stat[(size_t)hi.h * a.rows_q + sp.q0 + i] = lse2[nb];
+      stat[(size_t)(a.heads + hi.h) * a.rows_q + sp.q0 + i] = delta[nb];
+    }
+  }
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int i = iw + nb * 16 + l16;
