@@ -7,6 +7,7 @@ bfloat16 (DCHAG_BF16).  Each function has the name and the meaning of the C entr
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -463,7 +464,7 @@ def _row_stride(t: torch.Tensor, name: str) -> int:
     """Elements from one row to the next of [rows, heads, d] whose heads lie one behind the other."""
     rows, heads, d = t.shape
     row, head, one = t.stride()
-    if t.numel() and ((d > 1 and one != 1) or (heads > 1 and head != d)):
+    if ((d > 1 and one != 1) or (heads > 1 and head != d)) and t.numel():
         raise ValueError(f"the heads of a row of {name} must lie one behind the other")
     return row if rows > 1 else 0
 
@@ -472,7 +473,7 @@ def _addr(t: torch.Tensor, dtype: torch.dtype, device: int, name: str) -> int:
     """Address of a tensor of that type on the current device; its strides are the caller's business."""
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if not t.is_cuda or t.device.index != device:
+    if t.get_device() != device:
         raise ValueError(f"{name} must be a tensor on the current device")
     return t.data_ptr()
 
@@ -488,8 +489,24 @@ def _device(t: torch.Tensor) -> int:
     return torch.cuda.current_device()
 
 
-def _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders, device):
-    """The C struct of a call, and what it points to on the host."""
+def _raw_stream(device: int) -> int:
+    """The current stream's handle, without making a stream object of it, which would take longer than the rest of a call."""
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _on_stream(call):
+    """Makes a call on the stream it is given, if it is given one: what the call allocates then is that stream's, too."""
+    @functools.wraps(call)
+    def on_stream(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        with torch.cuda.stream(stream):
+            return call(*args, **kw)
+    return on_stream
+
+
+def _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders, device, others=(0, 0, 0, 0, 0)):
+    """The C struct of a call, and what it points to on the host; others: row strides of out, dout, dq, dk, dv."""
     if q.dim() != 3 or k.dim() != 3 or v.shape != k.shape:
         raise ValueError("q must be [rows, heads, head_dim], k and v [rows, kv_heads, head_dim]")
     rows_q, heads, d = q.shape
@@ -501,27 +518,27 @@ def _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders
     sequences = q_starts.shape[0] - 1
     _vector(q_starts, sequences + 1, "q_starts")
     _vector(k_starts, sequences + 1, "k_starts")
-    a = _CAttention()
-    a.heads, a.kv_heads, a.head_dim, a.causal, a.sequences = heads, kv_heads, d, 1 if causal else 0, sequences
-    a.rows_q, a.rows_k, a.scale = rows_q, rows_k, scale
-    a.ld_q, a.ld_k, a.ld_v = _row_stride(q, "q"), _row_stride(k, "k"), _row_stride(v, "v")
-    a.q_starts = _addr(q_starts, torch.int32, device, "q_starts")
-    a.k_starts = _addr(k_starts, torch.int32, device, "k_starts")
+    used = host = bias_at = None
+    n = 0
     if k_used is not None:
         _vector(k_used, sequences, "k_used")
-        a.k_used = _addr(k_used, torch.int32, device, "k_used")
+        used = _addr(k_used, torch.int32, device, "k_used")
     if (bias is None) != (borders is None):
         raise ValueError("bias and borders come together")
-    if bias is None:
-        return a, None
-    n = len(borders)
-    if tuple(bias.shape) != (heads, (n + 1) * (1 if causal else 2)) or not bias.is_contiguous():
-        raise ValueError("bias must be contiguous, [heads, buckets] with one bucket more than borders, twice as many if not causal")
-    host = (ctypes.c_int32 * max(1, n))(*borders)
-    a.bias, a.n_borders, a.borders = _addr(bias, q.dtype, device, "bias"), n, ctypes.addressof(host)
+    if bias is not None:
+        n = len(borders)
+        if tuple(bias.shape) != (heads, (n + 1) * (1 if causal else 2)) or not bias.is_contiguous():
+            raise ValueError("bias must be contiguous, [heads, buckets] with one bucket more than borders, twice as many if not causal")
+        host = (ctypes.c_int32 * max(1, n))(*borders)
+        bias_at = _addr(bias, q.dtype, device, "bias")
+    a = _CAttention(heads, kv_heads, d, 1 if causal else 0, sequences, rows_q, rows_k, scale,
+                    _row_stride(q, "q"), _row_stride(k, "k"), _row_stride(v, "v"), *others,
+                    _addr(q_starts, torch.int32, device, "q_starts"), _addr(k_starts, torch.int32, device, "k_starts"), used, bias_at,
+                    None if host is None else ctypes.addressof(host), n)
     return a, host
 
 
+@_on_stream
 def dchag_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: torch.Tensor, k_starts: torch.Tensor, *,
                  causal: bool = False, scale: float = 0.0, k_used: Optional[torch.Tensor] = None,
                  bias: Optional[torch.Tensor] = None, borders: Optional[Sequence[int]] = None,
@@ -531,26 +548,29 @@ def dchag_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: to
     [rows_k, kv_heads, d], int32 starts [sequences + 1] on the device.  Rows of a tensor may have gaps between them (columns of a
     joint projection).  Rows of no sequence are not written: give an `out` of your own if they are read later."""
     device = _device(q)
-    a, host = _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders, device)
-    dt, dtype, lib = _dt(q), q.dtype, load_library()
-    if out is None:
-        out = torch.empty(q.shape, dtype=dtype, device=q.device)
-    else:
+    ld_out = 0
+    if out is not None:
         if out.shape != q.shape:
             raise ValueError("out must be shaped like q")
-        a.ld_out = _row_stride(out, "out")
+        ld_out = _row_stride(out, "out")
+    a, host = _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders, device, (ld_out, 0, 0, 0, 0))
+    dt, dtype, lib = _dt(q), q.dtype, load_library()
+    where = q.device
+    if out is None:
+        out = torch.empty(q.shape, dtype=dtype, device=where)
     if lse is None:
-        lse = torch.empty((a.heads, a.rows_q), dtype=torch.float32, device=q.device)
+        lse = torch.empty((a.heads, a.rows_q), dtype=torch.float32, device=where)
     elif tuple(lse.shape) != (a.heads, a.rows_q) or not lse.is_contiguous():
         raise ValueError("lse must be [heads, rows_q] and contiguous")
     if workspace is None:
-        workspace = _workspace(lib.dchag_attend_workspace_bytes(dt, a, 0), q.device)
+        workspace = _workspace(lib.dchag_attend_workspace_bytes(dt, a, 0), where)
     _check(lib.dchag_attend(dt, a, _addr(q, dtype, device, "q"), _addr(k, dtype, device, "k"), _addr(v, dtype, device, "v"),
                             _addr(out, dtype, device, "out"), _addr(lse, torch.float32, device, "lse"), workspace.data_ptr(),
-                            workspace.numel(), _stream(stream)))
+                            workspace.numel(), _raw_stream(device)))
     return out, lse
 
 
+@_on_stream
 def dchag_attend_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
                           dout: torch.Tensor, q_starts: torch.Tensor, k_starts: torch.Tensor, *, causal: bool = False,
                           scale: float = 0.0, k_used: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
@@ -561,31 +581,30 @@ def dchag_attend_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out
     """(dq, dk, dv, dbias or None) of <dout, dchag_attend(...)>; out and lse are those of the forward call with the same arguments.
     Rows of no sequence are not written."""
     device = _device(q)
-    a, host = _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders, device)
-    dt, dtype, lib = _dt(q), q.dtype, load_library()
+    dt, dtype, lib, where = _dt(q), q.dtype, load_library(), q.device
     if dq is None:
-        dq = torch.empty(q.shape, dtype=dtype, device=q.device)
+        dq = torch.empty(q.shape, dtype=dtype, device=where)
     if dk is None:
-        dk = torch.empty(k.shape, dtype=dtype, device=q.device)
+        dk = torch.empty(k.shape, dtype=dtype, device=where)
     if dv is None:
-        dv = torch.empty(k.shape, dtype=dtype, device=q.device)
+        dv = torch.empty(k.shape, dtype=dtype, device=where)
     if dbias is None and bias is not None and want_dbias:
-        dbias = torch.empty(bias.shape, dtype=dtype, device=q.device)
+        dbias = torch.empty(bias.shape, dtype=dtype, device=where)
     if dbias is not None and (bias is None or dbias.shape != bias.shape or not dbias.is_contiguous()):
         raise ValueError("dbias goes with a bias, is shaped like it and contiguous")
     if out.shape != q.shape or dout.shape != q.shape or dq.shape != q.shape or dk.shape != k.shape or dv.shape != k.shape:
         raise ValueError("out, dout and dq must be shaped like q, dk and dv like k")
+    a, host = _attention(q, k, v, q_starts, k_starts, causal, scale, k_used, bias, borders, device,
+                         (_row_stride(out, "out"), _row_stride(dout, "dout"), _row_stride(dq, "dq"), _row_stride(dk, "dk"), _row_stride(dv, "dv")))
     if tuple(lse.shape) != (a.heads, a.rows_q) or not lse.is_contiguous():
         raise ValueError("lse must be [heads, rows_q] and contiguous")
-    a.ld_out, a.ld_dout, a.ld_dq = _row_stride(out, "out"), _row_stride(dout, "dout"), _row_stride(dq, "dq")
-    a.ld_dk, a.ld_dv = _row_stride(dk, "dk"), _row_stride(dv, "dv")
     if workspace is None:
         workspace = _workspace(lib.dchag_attend_workspace_bytes(dt, a, 1), q.device)
     _check(lib.dchag_attend_backward(
         dt, a, _addr(q, dtype, device, "q"), _addr(k, dtype, device, "k"), _addr(v, dtype, device, "v"), _addr(out, dtype, device, "out"),
         _addr(lse, torch.float32, device, "lse"), _addr(dout, dtype, device, "dout"), _addr(dq, dtype, device, "dq"),
         _addr(dk, dtype, device, "dk"), _addr(dv, dtype, device, "dv"), None if dbias is None else _addr(dbias, dtype, device, "dbias"),
-        workspace.data_ptr(), workspace.numel(), _stream(stream)))
+        workspace.data_ptr(), workspace.numel(), _raw_stream(device)))
     return dq, dk, dv, dbias
 
 
@@ -601,6 +620,7 @@ def _codes8(codes: torch.Tensor, scales: torch.Tensor, rows: int, D: int) -> Non
         raise ValueError("codes must be [rows, D] and scales [rows, (D + 31) // 32], contiguous")
 
 
+@_on_stream
 def dchag_pack8(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """(codes uint8 [rows, D], scales uint8 [rows, (D + 31) // 32]): the rows of x in 8 bits, one exponent for every 32 values."""
     ld, (rows, D), device = _matrix(x, "x"), x.shape, _device(x)
@@ -610,10 +630,11 @@ def dchag_pack8(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: O
         scales = torch.empty((rows, (D + 31) // 32), dtype=torch.uint8, device=x.device)
     _codes8(codes, scales, rows, D)
     _check(load_library().dchag_pack8(_dt(x), rows, D, ld, _addr(x, x.dtype, device, "x"), _addr(codes, torch.uint8, device, "codes"),
-                                      _addr(scales, torch.uint8, device, "scales"), _stream(stream)))
+                                      _addr(scales, torch.uint8, device, "scales"), _raw_stream(device)))
     return codes, scales
 
 
+@_on_stream
 def dchag_unpack8(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
                   out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The rows that codes and scales (dchag_pack8) stand for."""
@@ -624,10 +645,11 @@ def dchag_unpack8(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype 
     elif tuple(out.shape) != (rows, D):
         raise ValueError("out must be [rows, D]")
     _check(load_library().dchag_unpack8(_dt(out), rows, D, _matrix(out, "out"), _addr(codes, torch.uint8, device, "codes"),
-                                        _addr(scales, torch.uint8, device, "scales"), _addr(out, out.dtype, device, "out"), _stream(stream)))
+                                        _addr(scales, torch.uint8, device, "scales"), _addr(out, out.dtype, device, "out"), _raw_stream(device)))
     return out
 
 
+@_on_stream
 def dchag_weight_grad8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, dW: Optional[torch.Tensor] = None,
                        db: Optional[torch.Tensor] = None, want_db: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
     """(dW [d_out, d_in], db [d_out] or None) of a linear layer: dy [rows, d_out], its input in 8 bits (dchag_pack8)."""
@@ -645,7 +667,7 @@ def dchag_weight_grad8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tens
         workspace = _workspace(lib.dchag_weight_grad8_workspace_bytes(dt, rows, d_out, d_in), dy.device)
     _check(lib.dchag_weight_grad8(dt, rows, d_out, d_in, ld, _addr(dy, dtype, device, "dy"), _addr(codes, torch.uint8, device, "codes"),
                                   _addr(scales, torch.uint8, device, "scales"), _addr(dW, dtype, device, "dW"),
-                                  None if db is None else _addr(db, dtype, device, "db"), workspace.data_ptr(), workspace.numel(), _stream(stream)))
+                                  None if db is None else _addr(db, dtype, device, "db"), workspace.data_ptr(), workspace.numel(), _raw_stream(device)))
     return dW, db
 
 

@@ -331,14 +331,25 @@ __device__ __forceinline__ void interleave_reads() {
   }
 }
 
-// Workgroup: NW wavefronts of 16 NB queries of one head; the keys pass by in tiles of 64, two tiles of K and V in LDS, the next
-// one on its way (direct-to-LDS) while one is worked on.
-template <typename T, int DP, int NB, int NW, bool BIAS>
+// Where there are too few rows for all SIMDs, two wavefronts (SPLIT = 2) share 16 NB rows: each takes half of every tile, and the second leaves
+// what it has in LDS for the first.  The place of a wavefront's accumulators there: 16 bytes a lane and block.
+template <int DB, int NB>
+struct Handover {
+  static constexpr int kBytes = (DB * NB * 4 + 2 * NB) * 64 * 4;
+  unsigned char* at;
+  int lane;
+  __device__ __forceinline__ f32x4& block(int b, int nb) const { return *reinterpret_cast<f32x4*>(at + ((b * NB + nb) * 64 + lane) * 16); }
+  __device__ __forceinline__ float& number(int i) const { return *reinterpret_cast<float*>(at + DB * NB * 1024 + (i * 64 + lane) * 4); }
+};
+
+// Workgroup: NW / SPLIT groups of 16 NB queries of one head, SPLIT wavefronts each; the keys pass by in tiles of 64, two tiles of K and V in
+// LDS, the next one on its way (direct-to-LDS) while one is worked on.
+template <typename T, int DP, int NB, int NW, int SPLIT, bool BIAS>
 __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend(AttendArgs a, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
                                                        T* __restrict__ out, float* __restrict__ lse) {
   typedef Tile<T, DP> TL;
   typedef typename Frag<T>::type frag;
-  constexpr int KS = DP / 32, DB = DP / 16, MB = kTileKeys / 16, ROWS = NW * NB * 16, NT = NW * 64;
+  constexpr int KS = DP / 32, DB = DP / 16, HALVES = 2 / SPLIT, MB = 2 * HALVES, ROWS = NW / SPLIT * NB * 16, NT = NW * 64;   // MB: of a wavefront's part of a tile
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float* table = reinterpret_cast<float*>(smem + 4 * TL::kBytes);
   const HeadItem hi = head_item(a, blockIdx.x);
@@ -346,7 +357,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend(Atte
   if (!find_span(a, hi.idx, [](int nq, int) { return (nq + ROWS - 1) / ROWS; }, sp)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
   const int i0 = (a.causal ? sp.tiles - 1 - sp.tile : sp.tile) * ROWS;      // causal: the longest rows first
-  const int iw = i0 + wave * NB * 16, off = sp.nk - sp.nq;
+  const int iw = i0 + wave / SPLIT * NB * 16, off = sp.nk - sp.nq, h0 = SPLIT == 2 ? wave & 1 : 0;
   const int kend = a.causal ? min(sp.nk, max(0, min(i0 + ROWS, sp.nq) + off)) : sp.nk;
   const int tiles = (kend + kTileKeys - 1) / kTileKeys;
   const T* kb_ = k + (long)sp.k0 * a.ld_k + hi.kvh * a.d;
@@ -399,7 +410,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend(Atte
       for (int nb = 0; nb < NB; ++nb) s[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const frag kf = TL::row_frag(K, mb, ks, lane);
+        const frag kf = TL::row_frag(K, h0 * 2 + mb, ks, lane);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) s[mb][nb] = mma(s[mb][nb], kf, qf[nb][ks]);
       }
@@ -414,7 +425,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend(Atte
         mul = 1.f;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const float* tb = table + kb + 4 * g - (lo + nb * 16 + l16) + a.last + kPad;
+          const float* tb = table + kb + h0 * 32 + 4 * g - (lo + nb * 16 + l16) + a.last + kPad;
 #pragma unroll
           for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -430,7 +441,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend(Atte
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (kb + mb * 16 + 4 * g + r >= end) s[mb][nb][r] = kNegInf;
+            if (kb + h0 * 32 + mb * 16 + 4 * g + r >= end) s[mb][nb][r] = kNegInf;
       }
     }
     float mx[NB];
@@ -453,7 +464,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend(Atte
         for (int b = 0; b < DB; ++b) acc[b][nb] *= f;
       }
     }
-    const bool slow = MASKED && any_not_finite<T, DP, kTileKeys>(V, 0, lane);
+    const bool slow = MASKED && any_not_finite<T, DP, 32 * HALVES>(V, h0 * 32, lane);
     auto exps = [&](int h2) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
@@ -468,30 +479,55 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend(Atte
     };
     exps(0);
 #pragma unroll
-    for (int h2 = 0; h2 < MB / 2; ++h2) {
+    for (int h2 = 0; h2 < HALVES; ++h2) {
       frag pf[NB];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int j = 0; j < 8; ++j) pf[nb][j] = (T)s[h2 * 2 + (j >> 2)][nb][j & 3];
-      if (h2 == 0) exps(1);
+      if constexpr (HALVES == 2)
+        if (h2 == 0) exps(1);
       if (MASKED && slow) {
-        accumulate_pairs<T, DP, NB>(acc, pf, V, h2 * 32, lane);
+        accumulate_pairs<T, DP, NB>(acc, pf, V, (h0 + h2) * 32, lane);
         continue;
       }
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
-        const frag vf = TL::col_frag(V, b, h2, lane);
+        const frag vf = TL::col_frag(V, b, h0 + h2, lane);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) acc[b][nb] = mma(acc[b][nb], vf, pf[nb]);
       }
     }
-    if (!MASKED) interleave_reads<T, DB * MB / 2, 2, NB, 3>();
+    if (!MASKED) interleave_reads<T, DB * HALVES, 2, NB, 3>();
   };
   const int full = min(sp.nk, a.causal ? max(0, i0 + off + 1) : sp.nk) / kTileKeys;         // tiles all of whose pairs are visible
   int t = 0;
   for (; t < min(full, tiles); ++t) step(t, std::false_type{});
   for (; t < tiles; ++t) step(t, std::true_type{});
+  if constexpr (SPLIT == 2) {
+    __syncthreads();
+    const Handover<DB, NB> there{smem + (wave >> 1) * Handover<DB, NB>::kBytes, lane};
+    if (h0) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        there.number(2 * nb) = m[nb];
+        there.number(2 * nb + 1) = l[nb];
+#pragma unroll
+        for (int b = 0; b < DB; ++b) there.block(b, nb) = acc[b][nb];
+      }
+    }
+    __syncthreads();
+    if (h0) return;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float other = there.number(2 * nb), next = fmaxf(m[nb], other);
+      const float f = __builtin_amdgcn_exp2f(m[nb] - next), fo = __builtin_amdgcn_exp2f(other - next);
+      m[nb] = next;
+      l[nb] = l[nb] * f + there.number(2 * nb + 1) * fo;
+#pragma unroll
+      for (int b = 0; b < DB; ++b) acc[b][nb] = acc[b][nb] * f + there.block(b, nb) * fo;
+    }
+  }
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int i = iw + nb * 16 + l16;
@@ -820,17 +856,18 @@ struct BiasGrad {
   }
 };
 
-template <typename T, int DP, int NB, int NW, bool BIAS>
+template <typename T, int DP, int NB, int NW, int SPLIT, bool BIAS>
 __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(AttendArgs a, const T* __restrict__ q, const T* __restrict__ k,
                                                       const T* __restrict__ v, const T* __restrict__ out, const float* __restrict__ lse,
                                                       const T* __restrict__ dout, T* __restrict__ dq, float* __restrict__ stat,
                                                       float* __restrict__ dbias_part, int want_dbias) {
   typedef Tile<T, DP> TL;
   typedef typename Frag<T>::type frag;
-  constexpr int KS = DP / 32, DB = DP / 16, ROWS = NW * NB * 16, NT = NW * 64;
+  constexpr int KS = DP / 32, DB = DP / 16, HALVES = 2 / SPLIT, ROWS = NW / SPLIT * NB * 16, NT = NW * 64;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
   const int entries = BIAS ? bias_table_size(a.last) : 0;
+  __shared__ float shared[NW][16];
   float* table = reinterpret_cast<float*>(smem + 4 * TL::kBytes);
   float* sums = table + ((entries + 3) & ~3) + wave * ((entries + 3) & ~3);
   float* pairs = table + ((entries + 3) & ~3) * (NW + 1) + wave * BiasGrad<NB>::kPairs;
@@ -843,7 +880,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
     return;
   }
   const int i0 = (a.causal ? sp.tiles - 1 - sp.tile : sp.tile) * ROWS;
-  const int iw = i0 + wave * NB * 16, off = sp.nk - sp.nq;
+  const int iw = i0 + wave / SPLIT * NB * 16, off = sp.nk - sp.nq, h0 = SPLIT == 2 ? wave & 1 : 0;
   const int kend = a.causal ? min(sp.nk, max(0, min(i0 + ROWS, sp.nq) + off)) : sp.nk;
   const int tiles = (kend + kTileKeys - 1) / kTileKeys;
   const T* kb_ = k + (long)sp.k0 * a.ld_k + hi.kvh * a.d;
@@ -935,6 +972,15 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
   };
   // -1, 1: all pairs of the tile are in the last bucket of that side
   auto side_of = [&](int kb) { return !BIAS ? 0 : kb + kTileKeys - 1 - lo <= -a.last ? -1 : kb - top >= a.last ? 1 : 0; };
+  // A row's number summed over the wavefronts that share it (every wavefront of the workgroup comes here).
+  auto both = [&](float v) {
+    if constexpr (SPLIT == 1) return v;
+    if (g == 0) shared[wave][l16] = v;
+    __syncthreads();
+    const float sum = shared[wave & ~1][l16] + shared[wave | 1][l16];
+    __syncthreads();
+    return sum;
+  };
   // delta from out as it was rounded to bf16 is off by up to 2^-8 <|do|, |out|>, which counts where few keys share a row's weight (dq's and dk's
   // error against 64 bits, 16 to 100 keys: 1.85 times that of the two roundings of P and dS alone).  So where a row has at most two tiles of
   // keys, which then both lie in LDS, it is added up from the pairs first: sum of P dP.
@@ -946,9 +992,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) sum[nb] = 0.f;
 #pragma unroll 1
-    for (int u = 0; u < 2 * tiles; ++u) {
+    for (int u = 0; u < HALVES * tiles; ++u) {
       f32x4 s[2][NB], dp[2][NB];
-      pairs_of(u >> 1, u & 1, std::true_type{}, s, dp, side_of((u >> 1) * kTileKeys));
+      const int t = u / HALVES;
+      pairs_of(t, h0 + u % HALVES, std::true_type{}, s, dp, side_of(t * kTileKeys));
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -957,7 +1004,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
           for (int r = 0; r < 4; ++r) sum[nb] = fmaf(s[mb][nb][r], dp[mb][nb][r], sum[nb]);
     }
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) delta[nb] = row_sum(sum[nb]);
+    for (int nb = 0; nb < NB; ++nb) delta[nb] = both(row_sum(sum[nb]));
   }
   // Bias gradient: rows' sums of dS, which delta's error alone makes differ from 0, and of P in the last bucket of each side; the error's share
   // of the last buckets is taken out at the end (2048 rows, 32 heads of 128: dbias' error against 64 bits 0.0031 -> 0.0016).
@@ -973,9 +1020,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
     if (iw >= sp.nq || (MASKED && a.causal && kb > top)) return;
     const unsigned char* K = smem + (t & 1) * 2 * TL::kBytes;
     const int side = side_of(kb);
-    const bool slow = MASKED && any_not_finite<T, DP, kTileKeys>(K, 0, lane);
+    const bool slow = MASKED && any_not_finite<T, DP, 32 * HALVES>(K, h0 * 32, lane);
 #pragma unroll
-    for (int h2 = 0; h2 < 2; ++h2) {
+    for (int hh = 0; hh < HALVES; ++hh) {
+      const int h2 = h0 + hh;
       f32x4 s[2][NB], dp[2][NB];
       pairs_of(t, h2, masked, s, dp, side);
       if (BIAS && want_dbias && side) {
@@ -1040,20 +1088,35 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
   for (int nb = 0; nb < NB; ++nb) {
     const int i = iw + nb * 16 + l16;
     if (BIAS && want_dbias) {
-      const float off_by = row_sum(rest[nb]);
+      const float off_by = both(row_sum(rest[nb]));
       sum_left -= off_by * far_p[nb][0];
       sum_right -= off_by * far_p[nb][1];
       delta[nb] += off_by;
     }
-    if (g == 0 && i < sp.nq) {
+    if (g == 0 && h0 == 0 && i < sp.nq) {
       stat[(size_t)hi.h * a.rows_q + sp.q0 + i] = lse2[nb];
       stat[(size_t)(a.heads + hi.h) * a.rows_q + sp.q0 + i] = delta[nb];
     }
   }
+  if constexpr (SPLIT == 2) {
+    __syncthreads();
+    const Handover<DB, NB> there{smem + (wave >> 1) * Handover<DB, NB>::kBytes, lane};
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+        if (h0) there.block(b, nb) = acc[b][nb];
+    __syncthreads();
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+        if (!h0) acc[b][nb] += there.block(b, nb);
+  }
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int i = iw + nb * 16 + l16;
-    if (i >= sp.nq) continue;
+    if (i >= sp.nq || h0) continue;
     T* o = dq + (long)(sp.q0 + i) * a.ld_dq + hi.h * a.d;
 #pragma unroll
     for (int b = 0; b < DB; ++b)
@@ -1103,20 +1166,21 @@ __global__ __launch_bounds__(64) void k_attend_dbias(int items, int entries, con
 template <typename T, int DP>
 constexpr int dkv_stage_bytes() { return 2 * Tile<T, DP>::kBytes + 2 * 64 * 4; }
 
-template <typename T, int DP, int NB, int NW, bool BIAS>
+template <typename T, int DP, int NB, int NW, int SPLIT, bool BIAS>
 __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(AttendArgs a, const T* __restrict__ q, const T* __restrict__ k,
                                                        const T* __restrict__ v, const T* __restrict__ dout, const float* __restrict__ stat,
                                                        T* __restrict__ dk, T* __restrict__ dv) {
   typedef Tile<T, DP> TL;
   typedef typename Frag<T>::type frag;
-  constexpr int KS = DP / 32, DB = DP / 16, ROWS = NW * NB * 16, NT = NW * 64, kStage = dkv_stage_bytes<T, DP>();
+  constexpr int KS = DP / 32, DB = DP / 16, HALVES = 2 / SPLIT, ROWS = NW / SPLIT * NB * 16, NT = NW * 64, kStage = dkv_stage_bytes<T, DP>();
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float* table = reinterpret_cast<float*>(smem + 2 * kStage);
   const int group = a.heads / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
   Span sp;
   if (!find_span(a, blockIdx.x / a.kv_heads, [](int, int nk) { return (nk + ROWS - 1) / ROWS; }, sp)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
-  const int j0 = sp.tile * ROWS, jw = j0 + wave * NB * 16, jtop = jw + NB * 16 - 1, off = sp.nk - sp.nq;
+  const int j0 = sp.tile * ROWS, jw = j0 + wave / SPLIT * NB * 16, jtop = jw + NB * 16 - 1, off = sp.nk - sp.nq;
+  const int h0 = SPLIT == 2 ? wave & 1 : 0;                                  // SPLIT = 2: of every tile, the half that this wavefront takes
   const int first = a.causal ? max(0, j0 - off) / kTileKeys : 0, per = max(0, (sp.nq + kTileKeys - 1) / kTileKeys - first);
   const int steps = per * group;
   auto stage = [&](int it) {
@@ -1165,9 +1229,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(
     int side = 0;
     if (BIAS) side = jtop - lo <= -a.last ? -1 : (jw - top >= a.last ? 1 : 0);
     const float far = side < 0 ? far_left : side > 0 ? far_right : 0.f;
-    const bool slow = MASKED && (any_not_finite<T, DP, kTileKeys>(dO, 0, lane) || any_not_finite<T, DP, kTileKeys>(Q, 0, lane));
+    const bool slow = MASKED && (any_not_finite<T, DP, 32 * HALVES>(dO, h0 * 32, lane) || any_not_finite<T, DP, 32 * HALVES>(Q, h0 * 32, lane));
 #pragma unroll
-    for (int h2 = 0; h2 < 2; ++h2) {
+    for (int hh = 0; hh < HALVES; ++hh) {
+      const int h2 = h0 + hh;
       frag pf[NB], df[NB];
 #pragma unroll
       for (int mb = 0; mb < 2; ++mb) {
@@ -1234,10 +1299,28 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dkv(
       while (tile < whole) step(it++, tile++, std::false_type{});
     }
   }
+  if constexpr (SPLIT == 2) {
+    const Handover<DB, NB> there{smem + (wave >> 1) * Handover<DB, NB>::kBytes, lane};
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      __syncthreads();
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+          if (h0) there.block(b, nb) = which ? av[b][nb] : ak[b][nb];
+      __syncthreads();
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+          if (!h0) (which ? av : ak)[b][nb] += there.block(b, nb);
+    }
+  }
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int j = jw + nb * 16 + l16;
-    if (j >= sp.nk) continue;
+    if (j >= sp.nk || h0) continue;
     T* ok = dk + (long)(sp.k0 + j) * a.ld_dk + kvh * a.d;
     T* ov = dv + (long)(sp.k0 + j) * a.ld_dv + kvh * a.d;
 #pragma unroll

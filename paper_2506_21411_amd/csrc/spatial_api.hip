@@ -77,25 +77,32 @@ long tiles_bound(long total, long sequences, int rows) { return total / rows + s
 
 int padded_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
-// Rows of a workgroup: 16 nb a wavefront, nw wavefronts.
+// Rows of a workgroup: 16 nb for every `split` of its nw wavefronts.
 struct TileShape {
-  int nb, nw;
-  int rows() const { return 16 * nb * nw; }
+  int nb, nw, split;
+  int rows() const { return 16 * nb * nw / split; }
 };
-// Tiles of 64 rows where larger ones would leave compute units without work (and for fp32, whose fragments fill the registers); of 256 for
+// Where tiles of 128 rows would leave compute units without work: tiles of 32, two wavefronts to a row (64 rows gave every SIMD one wavefront:
+// training step, 4 x 256 rows, 16 heads of 64, kernels' us 44 / 36).  fp32, whose fragments fill the registers, has 16 rows a wavefront: tiles of
+// 64, or of 32 as above where 64 leave SIMDs with less than two wavefronts (2 x 512 rows, 8 heads of 64, us: 120 / 82).  bf16: tiles of 256 for
 // long sequences whose rows see every key (heads of more than 32: a tile of keys is a load for each of 512 threads); otherwise of 128, since a causal
-// tile's work grows with its rows and short sequences fill large tiles badly (eight of 77 to 2048 rows, us, 128 / 256: 55 / 74).  16 heads, 8192 rows, TFLOP/s with tiles
-// of 64 / 128 / 256: heads of 64 714 / 799 / 839, heads of 128 836 / 1107 / 1152; causal, 32 heads of 128 832 / 1069 / 1046.
+// tile's work grows with its rows and short sequences fill large tiles badly (eight of 77 to 2048 rows, us, 128 / 256: 55 / 74).
+// 16 heads, 8192 rows, TFLOP/s with tiles of 64 / 128 / 256: heads of 64 714 / 799 / 839, heads of 128 836 / 1107 / 1152; causal, 32 heads of 128
+// 832 / 1069 / 1046.
 TileShape tile_shape(dchag_dtype dt, int d, long rows, long sequences, long heads, bool causal) {
-  if (dt != DCHAG_BF16 || tiles_bound(rows, sequences, 128) * heads < compute_units()) return {1, 4};
-  if (causal || d <= 32 || rows < 1024 * sequences || tiles_bound(rows, sequences, 256) * heads < compute_units()) return {2, 4};
-  return {2, 8};
+  const long cus = compute_units();
+  if (dt != DCHAG_BF16) return {1, 4, tiles_bound(rows, sequences, 64) * heads < 2 * cus ? 2 : 1};
+  if (tiles_bound(rows, sequences, 128) * heads < cus) return {1, 4, 2};
+  if (causal || d <= 32 || rows < 1024 * sequences || tiles_bound(rows, sequences, 256) * heads < cus) return {2, 4, 1};
+  return {2, 8, 1};
 }
+
+template <int N> using Const = std::integral_constant<int, N>;
 
 // How a forward call goes about its rows: few (k_attend_few) or tiles of 64 nb rows.
 struct ForwardPlan {
   bool few;
-  int nb, nw;                 // 16 nb rows a wavefront, nw wavefronts a workgroup
+  TileShape tile;
   long items, stretches;      // row tiles at most; few: parts that they are dealt to, 0: not split
   size_t part, part_ml, total;
 };
@@ -118,17 +125,15 @@ ForwardPlan forward_plan(dchag_dtype dt, const AttendArgs& a) {
     }
     return p;
   }
-  const TileShape t = tile_shape(dt, a.d, a.rows_q, a.sequences, a.heads, a.causal);
-  p.nb = t.nb;
-  p.nw = t.nw;
-  p.items = tiles_bound(a.rows_q, a.sequences, t.rows());
+  p.tile = tile_shape(dt, a.d, a.rows_q, a.sequences, a.heads, a.causal);
+  p.items = tiles_bound(a.rows_q, a.sequences, p.tile.rows());
   return p;
 }
 
-template <typename T, int DP, int NB, int NW, bool BIAS>
+template <typename T, int DP, int NB, int NW, int SPLIT, bool BIAS>
 int launch_attend(const AttendArgs& a, const ForwardPlan& p, const void* q, const void* k, const void* v, void* out, float* lse, hipStream_t st) {
   const int lds = 4 * Tile<T, DP>::kBytes + (BIAS ? bias_table_size(a.last) * 4 : 0);
-  auto kern = k_attend<T, DP, NB, NW, BIAS>;
+  auto kern = k_attend<T, DP, NB, NW, SPLIT, BIAS>;
   if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
   StageTimer tm(DCHAG_STAGE_ATTEND, st);
   kern<<<dim3((unsigned)(p.items * a.heads)), NW * 64, lds, st>>>(a, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v),
@@ -160,13 +165,18 @@ template <typename T, int DP>
 int attend_dim(const AttendArgs& a, const ForwardPlan& p, const void* q, const void* k, const void* v, void* out, float* lse, unsigned char* ws,
                hipStream_t st) {
   if (p.few) return a.bias ? launch_few<T, DP, true>(a, p, q, k, v, out, lse, ws, st) : launch_few<T, DP, false>(a, p, q, k, v, out, lse, ws, st);
-  if constexpr (sizeof(T) == 2)
-    if (p.nb == 2) {
-      if constexpr (DP > 32)
-        if (p.nw == 8) return a.bias ? launch_attend<T, DP, 2, 8, true>(a, p, q, k, v, out, lse, st) : launch_attend<T, DP, 2, 8, false>(a, p, q, k, v, out, lse, st);
-      return a.bias ? launch_attend<T, DP, 2, 4, true>(a, p, q, k, v, out, lse, st) : launch_attend<T, DP, 2, 4, false>(a, p, q, k, v, out, lse, st);
-    }
-  return a.bias ? launch_attend<T, DP, 1, 4, true>(a, p, q, k, v, out, lse, st) : launch_attend<T, DP, 1, 4, false>(a, p, q, k, v, out, lse, st);
+  const auto go = [&](auto nb, auto nw, auto split) {
+    return a.bias ? launch_attend<T, DP, nb.value, nw.value, split.value, true>(a, p, q, k, v, out, lse, st)
+                  : launch_attend<T, DP, nb.value, nw.value, split.value, false>(a, p, q, k, v, out, lse, st);
+  };
+  if constexpr (sizeof(T) == 2) {
+    if constexpr (DP > 32)
+      if (p.tile.nw == 8) return go(Const<2>{}, Const<8>{}, Const<1>{});
+    if (p.tile.nb == 2) return go(Const<2>{}, Const<4>{}, Const<1>{});
+  } else {
+    if (p.tile.split == 1) return go(Const<1>{}, Const<4>{}, Const<1>{});
+  }
+  return go(Const<1>{}, Const<4>{}, Const<2>{});
 }
 
 struct BackwardPlan {
@@ -183,8 +193,8 @@ BackwardPlan backward_plan(dchag_dtype dt, const AttendArgs& a) {
   p.q = tile_shape(dt, a.d, a.rows_q, a.sequences, a.heads, a.causal);
   p.k = tile_shape(dt, a.d, a.rows_k, a.sequences, a.kv_heads, true);
   if (a.d > 64) {
-    if (a.bias && p.q.nb == 2) p.q = {1, 8};
-    p.k = {1, 4};
+    if (a.bias && p.q.nb == 2) p.q = {1, 8, 1};
+    if (p.k.nb == 2) p.k = {1, 4, 1};
   }
   p.items_q = tiles_bound(a.rows_q, a.sequences, p.q.rows());
   p.items_k = tiles_bound(a.rows_k, a.sequences, p.k.rows());
@@ -200,11 +210,11 @@ struct BackwardPtrs {
   void *dq, *dk, *dv, *dbias;
 };
 
-template <typename T, int DP, int NB, int NW, bool BIAS>
+template <typename T, int DP, int NB, int NW, int SPLIT, bool BIAS>
 int launch_dq(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
   const int table = (bias_table_size(a.last) + 3) & ~3;
   const int lds = 4 * Tile<T, DP>::kBytes + (BIAS ? table * 4 * (NW + 1) + NW * BiasGrad<NB>::kPairs * 4 : 0);
-  auto kern = k_attend_dq<T, DP, NB, NW, BIAS>;
+  auto kern = k_attend_dq<T, DP, NB, NW, SPLIT, BIAS>;
   if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
   StageTimer tm(DCHAG_STAGE_BWD_ATTEND_QUERY, st);
   if (p.items_q > 0)
@@ -214,10 +224,10 @@ int launch_dq(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t,
         t.dbias != nullptr);
   return launch_status();
 }
-template <typename T, int DP, int NB, int NW, bool BIAS>
+template <typename T, int DP, int NB, int NW, int SPLIT, bool BIAS>
 int launch_dkv(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
   const int lds = 2 * dkv_stage_bytes<T, DP>() + (BIAS ? bias_table_size(a.last) * 4 : 0);
-  auto kern = k_attend_dkv<T, DP, NB, NW, BIAS>;
+  auto kern = k_attend_dkv<T, DP, NB, NW, SPLIT, BIAS>;
   if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
   StageTimer tm(DCHAG_STAGE_BWD_ATTEND_KEY, st);
   if (p.items_k > 0)
@@ -229,20 +239,18 @@ int launch_dkv(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t
 
 template <typename T, int DP, bool BIAS>
 int backward_bias(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
+  const auto queries = [&](auto nb, auto nw, auto split) { return launch_dq<T, DP, nb.value, nw.value, split.value, BIAS>(a, p, t, ws, st); };
+  const auto keys = [&](auto nb, auto split) { return launch_dkv<T, DP, nb.value, 4, split.value, BIAS>(a, p, t, ws, st); };
   int rc;
-  if constexpr (sizeof(T) == 4) {
-    rc = launch_dq<T, DP, 1, 4, BIAS>(a, p, t, ws, st);
-    if (!rc) rc = launch_dkv<T, DP, 1, 4, BIAS>(a, p, t, ws, st);
-  } else {
-    if (p.q.nb == 1 && p.q.nw == 4) rc = launch_dq<T, DP, 1, 4, BIAS>(a, p, t, ws, st);
-    else if constexpr (DP == 128 && BIAS) rc = launch_dq<T, DP, 1, 8, BIAS>(a, p, t, ws, st);
-    else if constexpr (DP == 32) rc = launch_dq<T, DP, 2, 4, BIAS>(a, p, t, ws, st);
-    else rc = p.q.nw == 8 ? launch_dq<T, DP, 2, 8, BIAS>(a, p, t, ws, st) : launch_dq<T, DP, 2, 4, BIAS>(a, p, t, ws, st);
-    if (!rc) {
-      if constexpr (DP == 128) rc = launch_dkv<T, DP, 1, 4, BIAS>(a, p, t, ws, st);
-      else rc = p.k.nb == 2 ? launch_dkv<T, DP, 2, 4, BIAS>(a, p, t, ws, st) : launch_dkv<T, DP, 1, 4, BIAS>(a, p, t, ws, st);
-    }
-  }
+  if (p.q.split == 2) rc = queries(Const<1>{}, Const<4>{}, Const<2>{});
+  else if constexpr (sizeof(T) == 4) rc = queries(Const<1>{}, Const<4>{}, Const<1>{});
+  else if constexpr (DP == 128 && BIAS) rc = queries(Const<1>{}, Const<8>{}, Const<1>{});
+  else if constexpr (DP == 32) rc = queries(Const<2>{}, Const<4>{}, Const<1>{});
+  else rc = p.q.nw == 8 ? queries(Const<2>{}, Const<8>{}, Const<1>{}) : queries(Const<2>{}, Const<4>{}, Const<1>{});
+  if (rc) return rc;
+  if (p.k.split == 2) rc = keys(Const<1>{}, Const<2>{});
+  else if constexpr (sizeof(T) == 4 || DP == 128) rc = keys(Const<1>{}, Const<1>{});
+  else rc = keys(Const<2>{}, Const<1>{});
   if (rc || !BIAS || !t.dbias) return rc;
   StageTimer tm(DCHAG_STAGE_BWD_ATTEND_BIAS, st);
   const int entries = a.heads * a.buckets;

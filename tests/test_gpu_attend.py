@@ -110,16 +110,50 @@ def test_forward_and_backward(dtype, case):
     Problem(dtype, seed=11, **case).check()
 
 
-# rows enough for the larger tiles (128 rows of a workgroup): 2048 tiles at least on any device of up to 512 compute units
+# rows enough for the larger tiles (128 rows of a workgroup, 256 in the last two; fp32: 64) on a device of up to 256 compute units
 @pytest.mark.parametrize("case", [
     dict(heads=16, kv=16, d=64, ql=[129, 257, 1, 190] * 9, borders=LOG),
     dict(heads=16, kv=16, d=128, ql=[200, 77, 130, 65] * 9, causal=True),
     dict(heads=32, kv=16, d=32, ql=[200, 77, 130, 65] * 9, causal=True, borders=LOG),
     dict(heads=16, kv=16, d=128, ql=[200, 77, 130, 65] * 9, borders=[1, 4, 60]),
-], ids=["64", "128c", "32c", "128b"])
+    dict(heads=16, kv=4, d=64, ql=[129, 257, 1, 190] * 9, causal=True),
+    dict(dtype="f32", heads=16, kv=8, d=64, ql=[129, 257, 1, 190] * 5, borders=LOG),
+    dict(dtype="f32", heads=16, kv=16, d=128, ql=[129, 257, 1, 190] * 5, causal=True),
+    dict(heads=32, kv=8, d=64, ql=[1100, 1030], borders=[1, 2, 70, 300]),
+    dict(heads=32, kv=32, d=128, ql=[1030, 1100]),
+], ids=["64", "128c", "32c", "128b", "64c", "f32", "f32c", "256", "256w"])
 def test_large_tiles(case):
-    say(f"attention, tiles of 128 rows {case}")
-    Problem("bf16", seed=12, **case).check()
+    say(f"attention, large tiles {case}")
+    Problem(**{"dtype": "bf16", "seed": 12, **case}).check()
+
+
+@pytest.mark.parametrize("few", [False, True])
+def test_more_sequences_than_lanes(few):
+    """150 sequences, some empty: a wavefront looks its sequence up 64 at a time."""
+    gen = torch.Generator().manual_seed(40)
+    kl = [int(x) for x in torch.randint(0, 2600 if few else 60, (150,), generator=gen)]
+    ql = [int(x) for x in torch.randint(0, 3, (150,), generator=gen)] if few else [x + int(y) for x, y in zip(kl, torch.randint(0, 40, (150,), generator=gen))]
+    Problem("bf16", 4 if few else 8, 2, 32, ql, kl, causal=True, borders=[1, 5, 30], seed=41, train=not few).check()
+
+
+@pytest.mark.parametrize("case", [dict(heads=4, kv=2, d=64, ql=[150, 70]), dict(heads=8, kv=2, d=64, ql=[1, 1], kl=[4000, 1000])], ids=["tiles", "few"])
+def test_a_stream_of_its_own(case):
+    """stream=: work, workspaces and results are that stream's, whatever the current one is busy with."""
+    p = Problem("bf16", causal=True, seed=42, tail=0, **case)
+    want = p.run()
+    q, k, v, dout, kw, qs, ks = p.q.cuda(), p.k.cuda(), p.v.cuda(), p.dout.cuda(), p.kw(), dev(p.qs), dev(p.ks)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy = torch.randn((2048, 2048), device="cuda")
+    got = []
+    for _ in range(6):
+        busy = (busy @ busy).clamp(-1, 1)                          # allocates and frees on the current stream
+        out, lse = dchag.dchag_attend(q, k, v, qs, ks, stream=side, **kw)
+        got.append([out, lse, *dchag.dchag_attend_backward(q, k, v, out, lse, dout, qs, ks, stream=side, **kw)[:3]])
+    torch.cuda.synchronize()
+    for g in got:
+        for name, t in zip(("out", "lse", "dq", "dk", "dv"), g):
+            assert torch.equal(t, want[name]), name
 
 
 FEW = [
