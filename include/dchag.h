@@ -329,7 +329,8 @@ size_t dchag_workspace_bytes(dchag_dtype dt, int B, int C, int H, int W, int p, 
  *
  * The bias is learned per head and bucket of relative positions: bucket(r) = the number of borders <= |r|, plus
  * n_borders + 1 if r > 0 and the call is not causal.  So bias is [heads][buckets] with buckets = n_borders + 1 (causal) or
- * 2 (n_borders + 1).  An entry at or below -1e30 masks its pairs.
+ * 2 (n_borders + 1).  An entry at or below -1e30 masks its pairs (they weigh nothing, but unlike pairs that are not visible their
+ * values have to be finite).
  */
 typedef struct {
   int32_t heads, kv_heads;          /* kv_heads divides heads                                            */
@@ -349,7 +350,7 @@ typedef struct {
 } dchag_attention;
 
 /*
- * Forward pass.  workspace: dchag_attend_workspace_bytes(dt, att, 0) bytes, 256-byte aligned.
+ * Forward pass.  out may not overlap the inputs.  workspace: dchag_attend_workspace_bytes(dt, att, 0) bytes, 256-byte aligned.
  * Results do not depend on what other sequences a call holds, nor on how often it runs, up to the choice of kernel, which
  * goes by rows_q, rows_k, sequences and the head counts.
  * Errors: NULL att, starts, or a tensor that has rows; heads % kv_heads; head_dim; row strides; borders (DCHAG_ERR_SHAPE).
@@ -393,7 +394,7 @@ int dchag_unpack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void *c
  *
  *   dy [rows][d_out] with ld elements from row to row (0: d_out)    codes, scales of dchag_pack8 with D = d_in    dW [d_out][d_in]
  * workspace: dchag_weight_grad8_workspace_bytes(...) bytes.  Sums are fp32 in a fixed order.
- * Errors: NULL pointers; d_out, d_in % 8 != 0 or < 8; ld as above; rows < 0.  rows = 0 gives zeros.
+ * Errors: NULL pointers; d_out, d_in % 8 != 0 or < 8; ld as above; rows < 0 or > 2^30.  rows = 0 gives zeros.
  */
 int dchag_weight_grad8(dchag_dtype dt, int rows, int d_out, int d_in, int64_t ld, const void *dy, const void *codes,
                        const void *scales, void *dW, void *db, void *workspace, size_t workspace_bytes, void *stream);

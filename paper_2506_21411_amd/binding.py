@@ -466,6 +466,8 @@ def _row_stride(t: torch.Tensor, name: str) -> int:
     row, head, one = t.stride()
     if ((d > 1 and one != 1) or (heads > 1 and head != d)) and t.numel():
         raise ValueError(f"the heads of a row of {name} must lie one behind the other")
+    if rows > 1 and row < heads * d:
+        raise ValueError(f"the rows of {name} must not overlap")
     return row if rows > 1 else 0
 
 
@@ -612,6 +614,8 @@ def _matrix(t: torch.Tensor, name: str) -> int:
     """Elements from one row to the next of a matrix whose rows have no gaps inside."""
     if t.dim() != 2 or (t.numel() and t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be a matrix with adjacent columns")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"the rows of {name} must not overlap")
     return int(t.stride(0)) if t.shape[0] > 1 else 0
 
 

@@ -188,12 +188,21 @@ struct BackwardPlan {
 // 32 heads, us, tiles of 16 x 4 / 32 x 4 / 32 x 8 / 16 x 8 rows: - / 342 / 153 / 143).  Key tiles of heads of 128 have 16 keys a wavefront, as two
 // sums and two operands of 32 do not fit either (4096 rows, 16 heads, us: 16 x 4 296, 16 x 8 291, 32 x 4 755; causal with
 // grouped heads, 10374 rows: 745, 867, 2905).
+// The bias gradient's sums by distance, one set a wavefront, may leave no room for that many of them (borders beyond 1000 and heads of 128; fp32 beyond 460):
+// then fewer.
+template <typename T, int DP, int NB, int NW>
+constexpr int dq_lds(int last) {
+  return 4 * Tile<T, DP>::kBytes + (last ? ((bias_table_size(last) + 3) & ~3) * 4 * (NW + 1) + NW * BiasGrad<NB>::kPairs * 4 : 0);
+}
+constexpr int kLdsLimit = 160 * 1024 - 1024;                                 // 1024: what the kernels have beside it
 BackwardPlan backward_plan(dchag_dtype dt, const AttendArgs& a) {
   BackwardPlan p;
   p.q = tile_shape(dt, a.d, a.rows_q, a.sequences, a.heads, a.causal);
   p.k = tile_shape(dt, a.d, a.rows_k, a.sequences, a.kv_heads, true);
   if (a.d > 64) {
     if (a.bias && p.q.nb == 2) p.q = {1, 8, 1};
+    if (p.q.nw == 8 && a.bias && dq_lds<bf16, 128, 1, 8>(a.last) > kLdsLimit) p.q = {1, 4, 2};
+    if (dt == DCHAG_F32 && a.bias && dq_lds<float, 128, 1, 4>(a.last) > kLdsLimit) p.q = {1, 2, 1};
     if (p.k.nb == 2) p.k = {1, 4, 1};
   }
   p.items_q = tiles_bound(a.rows_q, a.sequences, p.q.rows());
@@ -212,8 +221,7 @@ struct BackwardPtrs {
 
 template <typename T, int DP, int NB, int NW, int SPLIT, bool BIAS>
 int launch_dq(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
-  const int table = (bias_table_size(a.last) + 3) & ~3;
-  const int lds = 4 * Tile<T, DP>::kBytes + (BIAS ? table * 4 * (NW + 1) + NW * BiasGrad<NB>::kPairs * 4 : 0);
+  const int lds = dq_lds<T, DP, NB, NW>(BIAS ? a.last : 0);
   auto kern = k_attend_dq<T, DP, NB, NW, SPLIT, BIAS>;
   if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
   StageTimer tm(DCHAG_STAGE_BWD_ATTEND_QUERY, st);
@@ -237,17 +245,11 @@ int launch_dkv(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t
   return launch_status();
 }
 
+// What follows the queries' gradients: the keys', and the sum of the bias gradient's parts.
 template <typename T, int DP, bool BIAS>
-int backward_bias(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
-  const auto queries = [&](auto nb, auto nw, auto split) { return launch_dq<T, DP, nb.value, nw.value, split.value, BIAS>(a, p, t, ws, st); };
+int rest_of_backward(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
   const auto keys = [&](auto nb, auto split) { return launch_dkv<T, DP, nb.value, 4, split.value, BIAS>(a, p, t, ws, st); };
   int rc;
-  if (p.q.split == 2) rc = queries(Const<1>{}, Const<4>{}, Const<2>{});
-  else if constexpr (sizeof(T) == 4) rc = queries(Const<1>{}, Const<4>{}, Const<1>{});
-  else if constexpr (DP == 128 && BIAS) rc = queries(Const<1>{}, Const<8>{}, Const<1>{});
-  else if constexpr (DP == 32) rc = queries(Const<2>{}, Const<4>{}, Const<1>{});
-  else rc = p.q.nw == 8 ? queries(Const<2>{}, Const<8>{}, Const<1>{}) : queries(Const<2>{}, Const<4>{}, Const<1>{});
-  if (rc) return rc;
   if (p.k.split == 2) rc = keys(Const<1>{}, Const<2>{});
   else if constexpr (sizeof(T) == 4 || DP == 128) rc = keys(Const<1>{}, Const<1>{});
   else rc = keys(Const<2>{}, Const<1>{});
@@ -256,6 +258,22 @@ int backward_bias(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs
   const int entries = a.heads * a.buckets;
   k_attend_dbias<T><<<dim3(entries), 64, 0, st>>>((int)p.items_q, entries, reinterpret_cast<const float*>(ws + p.dbias), static_cast<T*>(t.dbias));
   return launch_status();
+}
+template <typename T, int DP, bool BIAS>
+int backward_bias(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
+  const auto queries = [&](auto nb, auto nw, auto split) { return launch_dq<T, DP, nb.value, nw.value, split.value, BIAS>(a, p, t, ws, st); };
+  int rc;
+  if constexpr (sizeof(T) == 4 && DP == 128 && BIAS)
+    if (p.q.nw == 2) {
+      rc = queries(Const<1>{}, Const<2>{}, Const<1>{});
+      return rc ? rc : rest_of_backward<T, DP, BIAS>(a, p, t, ws, st);
+    }
+  if (p.q.split == 2) rc = queries(Const<1>{}, Const<4>{}, Const<2>{});
+  else if constexpr (sizeof(T) == 4) rc = queries(Const<1>{}, Const<4>{}, Const<1>{});
+  else if constexpr (DP == 128 && BIAS) rc = queries(Const<1>{}, Const<8>{}, Const<1>{});
+  else if constexpr (DP == 32) rc = queries(Const<2>{}, Const<4>{}, Const<1>{});
+  else rc = p.q.nw == 8 ? queries(Const<2>{}, Const<8>{}, Const<1>{}) : queries(Const<2>{}, Const<4>{}, Const<1>{});
+  return rc ? rc : rest_of_backward<T, DP, BIAS>(a, p, t, ws, st);
 }
 template <typename T, int DP>
 int backward_dim(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
@@ -300,7 +318,7 @@ Rows8 rows8(int64_t rows, int D, int64_t ld) {
 unsigned rows8_grid(const Rows8& r, int turns) { return (unsigned)((r.rows * r.blocks * 4 + 256 * turns - 1) / (256 * turns)); }
 int check_grad8(dchag_dtype dt, int rows, int d_out, int d_in, int64_t ld) {
   if (dt != DCHAG_F32 && dt != DCHAG_BF16) return DCHAG_ERR_DTYPE;
-  if (rows < 0 || d_out < 8 || d_in < 8 || d_out % 8 || d_in % 8 || d_out > (1 << 20) || d_in > (1 << 20)) return DCHAG_ERR_SHAPE;
+  if (rows < 0 || rows > (1 << 30) || d_out < 8 || d_in < 8 || d_out % 8 || d_in % 8 || d_out > (1 << 20) || d_in > (1 << 20)) return DCHAG_ERR_SHAPE;
   if (ld != 0 && (ld < d_out || ld % 8 || ld > (1 << 23))) return DCHAG_ERR_SHAPE;
   if ((int64_t)((d_out + 63) / 64) * ((d_in + 63) / 64) > (1 << 22)) return DCHAG_ERR_SHAPE;
   return DCHAG_OK;

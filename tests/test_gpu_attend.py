@@ -127,6 +127,15 @@ def test_large_tiles(case):
     Problem(**{"dtype": "bf16", "seed": 12, **case}).check()
 
 
+@pytest.mark.parametrize("case", [dict(dtype="f32", heads=2, kv=2, ql=[300, 1200]), dict(dtype="bf16", heads=2, kv=1, ql=[300, 1200]),
+                                  dict(dtype="bf16", heads=32, kv=32, ql=[1100, 1100])], ids=["f32", "bf16", "bf16 many"])
+@pytest.mark.parametrize("causal", [False, True])
+def test_borders_as_far_as_they_go(case, causal):
+    """The bias gradient's sums by distance at their longest, heads of 128: they leave room for fewer wavefronts."""
+    say(f"far borders {case} {causal}")
+    Problem(d=128, causal=causal, borders=[1, 2, 500, 1023, 1024], seed=43, **case).check()
+
+
 @pytest.mark.parametrize("few", [False, True])
 def test_more_sequences_than_lanes(few):
     """150 sequences, some empty: a wavefront looks its sequence up 64 at a time."""

@@ -112,7 +112,7 @@ def test_binding_refuses_what_the_library_cannot_see():
     q, k = torch.zeros(6, 4, 64), torch.zeros(6, 2, 64)
     s = torch.zeros(2, dtype=torch.int32)
     for args, kw in (((q[0], k, k, s, s), {}), ((q, k, k[:5], s, s), {}), ((q, k[..., :32], k[..., :32], s, s), {}),
-                     ((q.transpose(0, 1), k, k, s, s), {}), ((q, k, k, s, s[:1]), {}), ((q, k, k, s[None], s), {}),
+                     ((q.transpose(0, 1), k, k, s, s), {}), ((q[:1].expand(6, 4, 64), k, k, s, s), {}), ((q, k, k, s, s[:1]), {}), ((q, k, k, s[None], s), {}),
                      ((q, k, k, s, s), dict(bias=torch.zeros(4, 4))), ((q, k, k, s, s), dict(borders=[1])),
                      ((q, k, k, s, s), dict(bias=torch.zeros(4, 3), borders=[1])), ((q, k, k, s, s), {})):   # the last: not on a device
         with pytest.raises(ValueError):
@@ -121,6 +121,8 @@ def test_binding_refuses_what_the_library_cannot_see():
         dchag.dchag_pack8(torch.zeros(4, 8, 2))
     with pytest.raises(ValueError):
         dchag.dchag_pack8(torch.zeros(8, 8).t()[:, ::2])
+    with pytest.raises(ValueError):
+        dchag.dchag_pack8(torch.zeros(1, 8).expand(4, 8))
     with pytest.raises(ValueError):
         dchag.dchag_weight_grad8(torch.zeros(4, 8), torch.zeros((4, 64), dtype=torch.uint8), torch.zeros((4, 1), dtype=torch.uint8))
 
