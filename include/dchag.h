@@ -445,7 +445,8 @@ typedef enum {
   DCHAG_STAGE_BWD_ATTEND_BIAS = 26,/* the bias gradient's parts summed                         */
   DCHAG_STAGE_PACK8 = 27,          /* activations to 8 bits                                    */
   DCHAG_STAGE_UNPACK8 = 28,        /* and back                                                 */
-  DCHAG_STAGE_WEIGHT_GRAD8 = 29    /* weight gradient of a linear layer with an 8-bit input    */
+  DCHAG_STAGE_WEIGHT_GRAD8 = 29,   /* weight gradient of a linear layer with an 8-bit input    */
+  DCHAG_STAGE_ATTEND_PLAN = 30     /* which sequence a workgroup takes, for many sequences     */
 } dchag_stage;
 
 typedef struct {

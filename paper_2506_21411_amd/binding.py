@@ -58,7 +58,7 @@ STAGE_NAMES = {0: "tokenize", 1: "query", 2: "fold", 3: "scores", 4: "vproj", 5:
                12: "bwd_oproj", 13: "bwd_value", 14: "bwd_softmax", 15: "bwd_tokens", 16: "bwd_key_query",
                17: "bwd_tokenize", 18: "bwd_channel_mix", 19: "fold_value", 20: "tokenize_attend", 21: "key_prep",
                22: "attend", 23: "attend_join", 24: "bwd_attend_query", 25: "bwd_attend_key", 26: "bwd_attend_bias", 27: "pack8",
-               28: "unpack8", 29: "weight_grad8"}
+               28: "unpack8", 29: "weight_grad8", 30: "attend_plan"}
 
 LEVEL_ATTENTION, LEVEL_LINEAR = 0, 1
 

@@ -36,6 +36,7 @@ constexpr float kMaxSlack = 8.f;
 
 struct AttendArgs {
   const int *q_starts, *k_starts, *k_used;
+  const int* firsts;                   // of each sequence its first item, [sequences + 1] (k_attend_plan), or NULL: found in the kernel
   int sequences, rows_q, rows_k, heads, kv_heads, d, causal;
   long ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;   // elements from one row to the next
   float scale, c;                      // c = scale * log2(e)
@@ -205,11 +206,33 @@ __device__ __forceinline__ void read_span(const AttendArgs& a, int s, int& q0, i
   nk = min(max(a.k_starts[s + 1], k0), a.rows_k) - k0;
   if (a.k_used) nk = min(max(a.k_used[s], 0), nk);
 }
-// The sequence and tile that item idx is, the items of a sequence being count(nq, nk): 64 sequences at a time, one a lane.
-// False if there are not as many items.  Every wavefront finds it for itself.
+// The sequence that item `at` belongs to: the last one whose first item is not behind it.  64 places are looked at in one turn.
+__device__ __forceinline__ int find_sequence(const int* firsts, int sequences, int at) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = sequences;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, i = lo + (lane + 1) * step;
+    const bool behind = i < hi && firsts[i] <= at;
+    lo += __popcll(__ballot(behind)) * step;
+    hi = min(hi, lo + step);
+  }
+  return lo;
+}
+// The sequence and tile that item idx is, the items of a sequence being count(nq, nk).  False if there are not as many items.  Every wavefront finds
+// it for itself: up to kPlanFrom sequences by going through them 64 at a time, one a lane, beyond by a search in what k_attend_plan
+// has left (1024 sequences of 64 rows, 16 heads of 64, training step, us: 1262 / 701; 4096 single tokens against 128 keys: 4070 / 528).
+constexpr int kPlanFrom = 128;
 template <class Count>
 __device__ __forceinline__ bool find_span(const AttendArgs& a, int idx, Count count, Span& sp) {
   const int lane = threadIdx.x & 63;
+  if (a.firsts) {
+    if (idx >= a.firsts[a.sequences]) return false;
+    const int s = find_sequence(a.firsts, a.sequences, idx);
+    read_span(a, s, sp.q0, sp.nq, sp.k0, sp.nk);
+    sp.tiles = count(sp.nq, sp.nk);
+    sp.tile = idx - a.firsts[s];
+    return true;
+  }
   for (int s0 = 0; s0 < a.sequences; s0 += 64) {
     int q0 = 0, nq = 0, k0 = 0, nk = 0, n = 0;
     if (s0 + lane < a.sequences) {
@@ -564,8 +587,29 @@ __device__ __forceinline__ int wave_total(int v) {
   for (int w = 1; w < 64; w *= 2) v += __shfl_xor(v, w);
   return __builtin_amdgcn_readfirstlane(v);
 }
-// The stretch of index `at`, or (by_tile) the first one of row tile `at`; false if there are not as many.
+// The keys of a part, of `keys` in all row tiles together.
+__device__ __forceinline__ int part_keys(const AttendArgs& a, int stretches, int tiles, long keys) {
+  const int spare = stretches - tiles;
+  const long even = spare > 0 ? (keys + spare - 1) / spare : (long)a.rows_k + 1;
+  return (int)min(max((even + kFewKeys - 1) / kFewKeys * kFewKeys, 4L * kFewKeys), 1L << 30);
+}
+// The stretch of index `at`, or (by_tile) the first one of row tile `at`; false if there are not as many.  By a plan, the row tiles' first items lie
+// behind the stretches', and the keys of a part behind those.
 __device__ __forceinline__ bool find_stretch(const AttendArgs& a, int stretches, int at, bool by_tile, Stretch& st) {
+  if (a.firsts) {
+    const int *tiles = a.firsts + a.sequences + 1, *of = by_tile ? tiles : a.firsts, group = a.heads / a.kv_heads;
+    if (at >= of[a.sequences]) return false;
+    const int s = find_sequence(of, a.sequences, at);
+    st.keys = tiles[a.sequences + 1];
+    read_span(a, s, st.sp.q0, st.sp.nq, st.sp.k0, st.sp.nk);
+    st.sp.tiles = (st.sp.nq * group + kFewRows - 1) / kFewRows;
+    st.parts = max(1, (st.sp.nk + st.keys - 1) / st.keys);
+    const int inside = at - of[s];
+    st.sp.tile = by_tile ? inside : inside / st.parts;
+    st.part = by_tile ? 0 : inside % st.parts;
+    st.first = a.firsts[s] + st.sp.tile * st.parts;
+    return true;
+  }
   const int lane = threadIdx.x & 63, group = a.heads / a.kv_heads;
   long keys = 0;
   int tiles = 0;
@@ -578,9 +622,7 @@ __device__ __forceinline__ bool find_stretch(const AttendArgs& a, int stretches,
     keys += (long)wave_total(n * (nk >> 10)) << 10;                          // in 1024s and the rest: no 32-bit overflow
     keys += wave_total(n * (nk & 1023));
   }
-  const int spare = stretches - tiles;
-  const long even = spare > 0 ? (keys + spare - 1) / spare : (long)a.rows_k + 1;
-  st.keys = (int)min(max((even + kFewKeys - 1) / kFewKeys * kFewKeys, 4L * kFewKeys), 1L << 30);
+  st.keys = part_keys(a, stretches, tiles, keys);
   int first = 0;
   for (int s0 = 0; s0 < a.sequences; s0 += 64) {
     if (a.sequences > 64) {
@@ -621,6 +663,79 @@ __device__ __forceinline__ bool find_stretch(const AttendArgs& a, int stretches,
     first += __builtin_amdgcn_readlane(upto, 63);
   }
   return false;
+}
+
+// The first items of many sequences, for find_span (rows > 0: an item is a tile of so many query rows, or with block 1 of key_rows key rows,
+// into `keys`) and find_stretch (rows = 0).  A workgroup of 1024 threads a table; a thread takes a run of sequences.
+struct Total1024 {
+  int sums[16];
+  long keys[16];
+};
+__device__ __forceinline__ int scan1024(int v, int& total, int* sums) {     // the sum of the threads before, and of all
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int upto = v;
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) {
+    const int u = __shfl_up(upto, w);
+    if (lane >= w) upto += u;
+  }
+  __syncthreads();
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) before += sums[w];
+    total += sums[w];
+  }
+  return before + upto - v;
+}
+static __global__ __launch_bounds__(1024) void k_attend_plan(AttendArgs a, int rows, int key_rows, int stretches, int* __restrict__ firsts, int* __restrict__ keys) {
+  __shared__ Total1024 sh;
+  const int per = (a.sequences + 1023) / 1024, s0 = min((int)threadIdx.x * per, a.sequences), s1 = min(s0 + per, a.sequences);
+  const int group = a.heads / a.kv_heads;
+  const bool by_keys = blockIdx.x == 1;
+  int q0, nq, k0, nk, n = 0, total;
+  long some = 0;
+  for (int s = s0; s < s1; ++s) {
+    read_span(a, s, q0, nq, k0, nk);
+    const int t = by_keys ? (nk + key_rows - 1) / key_rows : rows ? (nq + rows - 1) / rows : (nq * group + kFewRows - 1) / kFewRows;
+    n += t;
+    some += (long)t * nk;
+  }
+  int at = scan1024(n, total, sh.sums);
+  int* to = by_keys ? keys : rows ? firsts : firsts + a.sequences + 1;
+  for (int s = s0; s < s1; ++s) {
+    to[s] = at;
+    read_span(a, s, q0, nq, k0, nk);
+    at += by_keys ? (nk + key_rows - 1) / key_rows : rows ? (nq + rows - 1) / rows : (nq * group + kFewRows - 1) / kFewRows;
+  }
+  if (threadIdx.x == 0) to[a.sequences] = total;
+  if (rows) return;
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) some += __shfl_xor(some, w);
+  if ((threadIdx.x & 63) == 0) sh.keys[threadIdx.x >> 6] = some;
+  __syncthreads();
+  long all = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) all += sh.keys[w];
+  const int part = part_keys(a, stretches, total, all);
+  n = 0;
+  for (int s = s0; s < s1; ++s) {
+    read_span(a, s, q0, nq, k0, nk);
+    n += (nq * group + kFewRows - 1) / kFewRows * max(1, (nk + part - 1) / part);
+  }
+  at = scan1024(n, total, sh.sums);
+  for (int s = s0; s < s1; ++s) {
+    firsts[s] = at;
+    read_span(a, s, q0, nq, k0, nk);
+    at += (nq * group + kFewRows - 1) / kFewRows * max(1, (nk + part - 1) / part);
+  }
+  if (threadIdx.x == 0) {
+    firsts[a.sequences] = total;
+    to[a.sequences + 1] = part;
+  }
 }
 
 template <typename T, int DP, bool BIAS>

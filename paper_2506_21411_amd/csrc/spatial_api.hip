@@ -75,6 +75,10 @@ AttendArgs kernel_args(const dchag_attention* a) {
 // Most tiles of `rows` rows that sequences of `total` rows can have.
 long tiles_bound(long total, long sequences, int rows) { return total / rows + std::min(sequences, total); }
 
+// Many sequences: tables of their first items, made by a launch of its own before the others.
+bool planned(const AttendArgs& a) { return a.sequences > kPlanFrom; }
+size_t plan_bytes(const AttendArgs& a, int tables) { return planned(a) ? align_up(((size_t)a.sequences + 2) * tables * 4) : 0; }
+
 int padded_dim(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
 // Rows of a workgroup: 16 nb for every `split` of its nw wavefronts.
@@ -104,7 +108,7 @@ struct ForwardPlan {
   bool few;
   TileShape tile;
   long items, stretches;      // row tiles at most; few: parts that they are dealt to, 0: not split
-  size_t part, part_ml, total;
+  size_t part, part_ml, plan, total;
 };
 ForwardPlan forward_plan(dchag_dtype dt, const AttendArgs& a) {
   ForwardPlan p;
@@ -112,7 +116,6 @@ ForwardPlan forward_plan(dchag_dtype dt, const AttendArgs& a) {
   const int group = a.heads / a.kv_heads;
   const long rows = (long)a.rows_q * group, seqs = std::min<long>(a.sequences, a.rows_q);
   p.few = rows <= 32L * seqs;
-  p.total = 256;
   if (p.few) {
     p.items = rows / kFewRows + std::min<long>(a.sequences, rows);
     const long fill = 4L * compute_units() / a.kv_heads;                     // twice the workgroups that the chip holds at once
@@ -121,12 +124,14 @@ ForwardPlan forward_plan(dchag_dtype dt, const AttendArgs& a) {
     if (split) {
       const size_t n = (size_t)p.stretches * a.kv_heads * kFewRows;
       p.part_ml = align_up(n * padded_dim(a.d) * 4);
-      p.total = p.part_ml + align_up(n * 8);
+      p.plan = p.part_ml + align_up(n * 8);
     }
+    p.total = p.plan + plan_bytes(a, 2) + 256;
     return p;
   }
   p.tile = tile_shape(dt, a.d, a.rows_q, a.sequences, a.heads, a.causal);
   p.items = tiles_bound(a.rows_q, a.sequences, p.tile.rows());
+  p.total = p.plan + plan_bytes(a, 1) + 256;
   return p;
 }
 
@@ -182,7 +187,7 @@ int attend_dim(const AttendArgs& a, const ForwardPlan& p, const void* q, const v
 struct BackwardPlan {
   TileShape q, k;
   long items_q, items_k;
-  size_t stat, dbias, total;
+  size_t stat, dbias, plan, total;
 };
 // Query tiles as in the forward pass, but with the bias gradient's sums a wavefront of 32 rows of a head of 128 does not fit its registers (2048 rows,
 // 32 heads, us, tiles of 16 x 4 / 32 x 4 / 32 x 8 / 16 x 8 rows: - / 342 / 153 / 143).  Key tiles of heads of 128 have 16 keys a wavefront, as two
@@ -209,7 +214,8 @@ BackwardPlan backward_plan(dchag_dtype dt, const AttendArgs& a) {
   p.items_k = tiles_bound(a.rows_k, a.sequences, p.k.rows());
   p.stat = 0;
   p.dbias = align_up((size_t)2 * a.heads * a.rows_q * 4);
-  p.total = p.dbias + align_up((size_t)p.items_q * a.heads * a.buckets * 4) + 256;
+  p.plan = p.dbias + align_up((size_t)p.items_q * a.heads * a.buckets * 4);
+  p.total = p.plan + plan_bytes(a, 2) + 256;
   return p;
 }
 
@@ -217,13 +223,15 @@ struct BackwardPtrs {
   const void *q, *k, *v, *out, *dout;
   const float* lse;
   void *dq, *dk, *dv, *dbias;
+  const int *firsts_q, *firsts_k;
 };
 
 template <typename T, int DP, int NB, int NW, int SPLIT, bool BIAS>
-int launch_dq(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
+int launch_dq(AttendArgs a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
   const int lds = dq_lds<T, DP, NB, NW>(BIAS ? a.last : 0);
   auto kern = k_attend_dq<T, DP, NB, NW, SPLIT, BIAS>;
   if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
+  a.firsts = t.firsts_q;
   StageTimer tm(DCHAG_STAGE_BWD_ATTEND_QUERY, st);
   if (p.items_q > 0)
     kern<<<dim3((unsigned)(p.items_q * a.heads)), NW * 64, lds, st>>>(
@@ -233,10 +241,11 @@ int launch_dq(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t,
   return launch_status();
 }
 template <typename T, int DP, int NB, int NW, int SPLIT, bool BIAS>
-int launch_dkv(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
+int launch_dkv(AttendArgs a, const BackwardPlan& p, const BackwardPtrs& t, unsigned char* ws, hipStream_t st) {
   const int lds = 2 * dkv_stage_bytes<T, DP>() + (BIAS ? bias_table_size(a.last) * 4 : 0);
   auto kern = k_attend_dkv<T, DP, NB, NW, SPLIT, BIAS>;
   if (ensure_dynamic_lds(reinterpret_cast<const void*>(kern), lds)) return DCHAG_ERR_LAUNCH;
+  a.firsts = t.firsts_k;
   StageTimer tm(DCHAG_STAGE_BWD_ATTEND_KEY, st);
   if (p.items_k > 0)
     kern<<<dim3((unsigned)(p.items_k * a.kv_heads)), NW * 64, lds, st>>>(
@@ -361,7 +370,7 @@ int dchag_attend(dchag_dtype dt, const dchag_attention* att, const void* q, cons
                  size_t workspace_bytes, void* stream) {
   int rc = check_attention(dt, att);
   if (rc) return rc;
-  const AttendArgs a = kernel_args(att);
+  AttendArgs a = kernel_args(att);
   if (a.rows_q > 0 && (!q || !out || !lse)) return DCHAG_ERR_NULL;
   if (a.rows_q > 0 && a.rows_k > 0 && (!k || !v)) return DCHAG_ERR_NULL;
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(lse)) return DCHAG_ERR_ALIGN;
@@ -372,6 +381,12 @@ int dchag_attend(dchag_dtype dt, const dchag_attention* att, const void* q, cons
   hipStream_t st = static_cast<hipStream_t>(stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   set_level(0);
+  if (planned(a)) {
+    int* firsts = reinterpret_cast<int*>(ws + p.plan);
+    StageTimer tm(DCHAG_STAGE_ATTEND_PLAN, st);
+    k_attend_plan<<<dim3(1), 1024, 0, st>>>(a, p.few ? 0 : p.tile.rows(), 0, (int)p.stretches, firsts, nullptr);
+    a.firsts = firsts;
+  }
   const int dp = padded_dim(a.d);
   if (dt == DCHAG_F32)
     return dp == 32 ? attend_dim<float, 32>(a, p, q, k, v, out, lse, ws, st)
@@ -384,7 +399,7 @@ int dchag_attend_backward(dchag_dtype dt, const dchag_attention* att, const void
                           const void* dout, void* dq, void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
   int rc = check_attention(dt, att);
   if (rc) return rc;
-  const AttendArgs a = kernel_args(att);
+  AttendArgs a = kernel_args(att);
   if (a.rows_q > 0 && (!q || !out || !lse || !dout || !dq)) return DCHAG_ERR_NULL;
   if (a.rows_k > 0 && (!k || !v || !dk || !dv)) return DCHAG_ERR_NULL;
   if (dbias && !att->bias) return DCHAG_ERR_SHAPE;
@@ -396,8 +411,15 @@ int dchag_attend_backward(dchag_dtype dt, const dchag_attention* att, const void
   if (p.items_q * a.heads > 0x7fffffffL || p.items_k * a.kv_heads > 0x7fffffffL) return DCHAG_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
-  const BackwardPtrs t{q, k, v, out, dout, lse, dq, dk, dv, dbias};
+  BackwardPtrs t{q, k, v, out, dout, lse, dq, dk, dv, dbias, nullptr, nullptr};
   set_level(0);
+  if (planned(a)) {
+    int* firsts = reinterpret_cast<int*>(ws + p.plan);
+    t.firsts_q = firsts;
+    t.firsts_k = firsts + a.sequences + 2;
+    StageTimer tm(DCHAG_STAGE_ATTEND_PLAN, st);
+    k_attend_plan<<<dim3(2), 1024, 0, st>>>(a, p.q.rows(), p.k.rows(), 0, firsts, firsts + a.sequences + 2);
+  }
   const int dp = padded_dim(a.d);
   if (dt == DCHAG_F32)
     return dp == 32 ? backward_dim<float, 32>(a, p, t, ws, st) : dp == 64 ? backward_dim<float, 64>(a, p, t, ws, st) : backward_dim<float, 128>(a, p, t, ws, st);

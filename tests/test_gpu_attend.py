@@ -137,12 +137,14 @@ def test_borders_as_far_as_they_go(case, causal):
 
 
 @pytest.mark.parametrize("few", [False, True])
-def test_more_sequences_than_lanes(few):
-    """150 sequences, some empty: a wavefront looks its sequence up 64 at a time."""
+@pytest.mark.parametrize("n", [100, 150, 1100])
+def test_more_sequences_than_lanes(few, n):
+    """Sequences by the hundred, some empty: a wavefront looks its own up 64 at a time, or in a table made for the call."""
     gen = torch.Generator().manual_seed(40)
-    kl = [int(x) for x in torch.randint(0, 2600 if few else 60, (150,), generator=gen)]
-    ql = [int(x) for x in torch.randint(0, 3, (150,), generator=gen)] if few else [x + int(y) for x, y in zip(kl, torch.randint(0, 40, (150,), generator=gen))]
-    Problem("bf16", 4 if few else 8, 2, 32, ql, kl, causal=True, borders=[1, 5, 30], seed=41, train=not few).check()
+    most = (2600 if n < 1000 else 40) if few else 60 if n < 1000 else 12
+    kl = [int(x) for x in torch.randint(0, most, (n,), generator=gen)]
+    ql = [int(x) for x in torch.randint(0, 3, (n,), generator=gen)] if few else [x + int(y) for x, y in zip(kl, torch.randint(0, 40, (n,), generator=gen))]
+    Problem("bf16", 4 if few else 8, 2, 32, ql, kl, causal=True, borders=[1, 5, 30], seed=41, train=not few or n > 1000).check()
 
 
 @pytest.mark.parametrize("case", [dict(heads=4, kv=2, d=64, ql=[150, 70]), dict(heads=8, kv=2, d=64, ql=[1, 1], kl=[4000, 1000])], ids=["tiles", "few"])
