@@ -568,7 +568,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend(Atte
 // the group), so that a key head's rows are read once for its whole group, and the keys are dealt out: to workgroups in
 // stretches, inside one to its wavefronts tile by tile.  A wavefront streams its tiles of 32 keys through LDS of its own, without
 // a barrier, the next K on its way while V is worked on and the reverse; what the wavefronts have is joined in LDS, what the workgroups have by k_attend_join.  HBM-bound.
-constexpr int kFewRows = 16, kFewKeys = 32;
+constexpr int kFewRows = 16;
+constexpr int kFewKeys = 32;
 template <typename T, int DP>
 constexpr int few_waves() { return DP * (int)sizeof(T) > 256 ? 2 : 4; }
 template <typename T, int DP>

@@ -87,7 +87,7 @@ struct TileShape {
   int rows() const { return 16 * nb * nw / split; }
 };
 // Where tiles of 128 rows would leave compute units without work: tiles of 32, two wavefronts to a row (64 rows gave every SIMD one wavefront:
-// training step, 4 x 256 rows, 16 heads of 64, kernels' us 44 / 36).  fp32, whose fragments fill the registers, has 16 rows a wavefront: tiles of
+// training step, 4 x 256 rows, 16 heads of 64, kernels' us 44 / 36), and for sequences that they hold whole (2048 of 24 rows, us: 1193 / 915).  fp32, whose fragments fill the registers, has 16 rows a wavefront: tiles of
 // 64, or of 32 as above where 64 leave SIMDs with less than two wavefronts (2 x 512 rows, 8 heads of 64, us: 120 / 82).  bf16: tiles of 256 for
 // long sequences whose rows see every key (heads of more than 32: a tile of keys is a load for each of 512 threads); otherwise of 128, since a causal
 // tile's work grows with its rows and short sequences fill large tiles badly (eight of 77 to 2048 rows, us, 128 / 256: 55 / 74).
@@ -96,7 +96,7 @@ struct TileShape {
 TileShape tile_shape(dchag_dtype dt, int d, long rows, long sequences, long heads, bool causal) {
   const long cus = compute_units();
   if (dt != DCHAG_BF16) return {1, 4, tiles_bound(rows, sequences, 64) * heads < 2 * cus ? 2 : 1};
-  if (tiles_bound(rows, sequences, 128) * heads < cus) return {1, 4, 2};
+  if (tiles_bound(rows, sequences, 128) * heads < cus || rows <= 32 * sequences) return {1, 4, 2};
   if (causal || d <= 32 || rows < 1024 * sequences || tiles_bound(rows, sequences, 256) * heads < cus) return {2, 4, 1};
   return {2, 8, 1};
 }
@@ -115,7 +115,10 @@ ForwardPlan forward_plan(dchag_dtype dt, const AttendArgs& a) {
   memset(&p, 0, sizeof p);
   const int group = a.heads / a.kv_heads;
   const long rows = (long)a.rows_q * group, seqs = std::min<long>(a.sequences, a.rows_q);
-  p.few = rows <= 32L * seqs;
+  // Few rows: on average at most as many as a row tile has, of grouped heads two tiles' (the other kernel reads the keys once a head), and
+  // many keys or hardly any rows.  us, few / tiles of 32 rows: 64 sequences, 2000 keys, 16 heads, 10 rows 104 / 105, 20 rows 133 / 106; 32 heads on 8,
+  // 5 rows 56 / 73; 2048 sequences of 10 rows and keys 200 / 132.
+  p.few = rows <= (group > 1 ? 2L : 1L) * kFewRows * seqs && (a.rows_k >= 128 * seqs || rows <= 4 * seqs);
   if (p.few) {
     p.items = rows / kFewRows + std::min<long>(a.sequences, rows);
     const long fill = 4L * compute_units() / a.kv_heads;                     // twice the workgroups that the chip holds at once
