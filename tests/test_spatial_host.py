@@ -167,7 +167,7 @@ def test_reference_against_the_library(causal):
 
 def test_reference_of_8_bits_against_the_library():
     """Codes of the format's definition against torch's e4m3 conversion, on every value of a grid with all its ties."""
-    x = torch.cat([torch.linspace(-448, 448, 30721), torch.linspace(-0.05, 0.05, 20481)])
+    x = torch.cat([torch.linspace(-448, 448, 28673), torch.linspace(-0.05, 0.05, 20481)])
     x = torch.nn.functional.pad(x, (0, -x.numel() % 8)).view(-1, 8)
     x = torch.cat([x, torch.full((x.shape[0], 24), 448.0)], 1)         # exponent 127 everywhere
     values, codes, held = ref.pack8(x)
