@@ -1039,8 +1039,8 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
   }
   const int lo = iw + off, top = lo + NB * 16 - 1;
   // P (into s) and dP of 32 keys of tile t, the second half of it if h2; P of a pair that is not visible is 0, and so is its dP.
-  auto pairs_of = [&](int t, int h2, auto masked, f32x4 (&s)[2][NB], f32x4 (&dp)[2][NB], int side) {
-    constexpr bool MASKED = decltype(masked)::value;
+  auto pairs_of = [&](int t, int h2, auto masked, auto near, f32x4 (&s)[2][NB], f32x4 (&dp)[2][NB], int side) {
+    constexpr bool MASKED = decltype(masked)::value, NEAR = BIAS && decltype(near)::value;
     const unsigned char* K = smem + (t & 1) * 2 * TL::kBytes;
     const unsigned char* V = K + TL::kBytes;
     const int kb = t * kTileKeys;
@@ -1062,7 +1062,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
       }
     }
     interleave_reads<T, 4 * KS, 1, NB, 4>();
-    if (BIAS && !side) {
+    if (NEAR && !side) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const float* tb = table + kb + h2 * 32 + 4 * g - (lo + nb * 16 + l16) + a.last + kPad;
@@ -1072,7 +1072,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
           for (int r = 0; r < 4; ++r) s[mb][nb][r] = fmaf(s[mb][nb][r], a.c, tb[mb * 16 + r]);
       }
     }
-    const float mul = BIAS && !side ? 1.f : a.c, far = side < 0 ? far_left : side > 0 ? far_right : 0.f;
+    const float mul = NEAR && !side ? 1.f : a.c, far = side < 0 ? far_left : side > 0 ? far_right : 0.f;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const float sub = far - lse2[nb];
@@ -1111,7 +1111,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
     for (int u = 0; u < HALVES * tiles; ++u) {
       f32x4 s[2][NB], dp[2][NB];
       const int t = u / HALVES;
-      pairs_of(t, h0 + u % HALVES, std::true_type{}, s, dp, side_of(t * kTileKeys));
+      pairs_of(t, h0 + u % HALVES, std::true_type{}, std::true_type{}, s, dp, side_of(t * kTileKeys));
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -1127,21 +1127,22 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
   float rest[NB], far_p[NB][2];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) rest[nb] = far_p[nb][0] = far_p[nb][1] = 0.f;
-  auto step = [&](int t, auto masked) {                                      // as in k_attend
-    constexpr bool MASKED = decltype(masked)::value;
+  auto step = [&](int t, auto masked, auto near) {                           // as in k_attend; near: some pair may need the table
+    constexpr bool MASKED = decltype(masked)::value, NEAR = decltype(near)::value;
     wait_vmcnt<0>();
     __syncthreads();
     if (t + 1 < tiles) stage(t + 1);
     const int kb = t * kTileKeys;
     if (iw >= sp.nq || (MASKED && a.causal && kb > top)) return;
     const unsigned char* K = smem + (t & 1) * 2 * TL::kBytes;
-    const int side = side_of(kb);
+    int side = side_of(kb);
+    if (!NEAR && BIAS) side = side < 0 ? -1 : 1;
     const bool slow = MASKED && any_not_finite<T, DP, 32 * HALVES>(K, h0 * 32, lane);
 #pragma unroll
     for (int hh = 0; hh < HALVES; ++hh) {
       const int h2 = h0 + hh;
       f32x4 s[2][NB], dp[2][NB];
-      pairs_of(t, h2, masked, s, dp, side);
+      pairs_of(t, h2, masked, near, s, dp, side);
       if (BIAS && want_dbias && side) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -1168,7 +1169,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
           rest[nb] += sum;
           all += sum;
         }
-        if (side) {
+        if (!NEAR || side) {
           if (side < 0) sum_left += all;
           else sum_right += all;
         } else {
@@ -1197,9 +1198,15 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
     }
   };
   const int full = min(sp.nk, a.causal ? max(0, i0 + off + 1) : sp.nk) / kTileKeys;
+  // tiles all of whose pairs with the workgroup's rows are in the last bucket: those before `left`, those from `right` on
+  const int left = max(0, i0 + off - a.last + 1) / kTileKeys, right = (max(0, i0 + ROWS - 1 + off + a.last) + kTileKeys - 1) / kTileKeys;
   int t = 0;
-  for (; t < min(full, tiles); ++t) step(t, std::false_type{});
-  for (; t < tiles; ++t) step(t, std::true_type{});
+  if (BIAS) {
+    for (; t < min(left, min(full, tiles)); ++t) step(t, std::false_type{}, std::false_type{});
+    for (; t < min(right, min(full, tiles)); ++t) step(t, std::false_type{}, std::true_type{});
+  }
+  for (; t < min(full, tiles); ++t) step(t, std::false_type{}, std::false_type{});
+  for (; t < tiles; ++t) step(t, std::true_type{}, std::true_type{});
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int i = iw + nb * 16 + l16;

@@ -192,11 +192,11 @@ struct BackwardPlan {
   long items_q, items_k;
   size_t stat, dbias, plan, total;
 };
-// Query tiles as in the forward pass, but with the bias gradient's sums a wavefront of 32 rows of a head of 128 does not fit its registers (2048 rows,
-// 32 heads, us, tiles of 16 x 4 / 32 x 4 / 32 x 8 / 16 x 8 rows: - / 342 / 153 / 143).  Key tiles of heads of 128 have 16 keys a wavefront, as two
-// sums and two operands of 32 do not fit either (4096 rows, 16 heads, us: 16 x 4 296, 16 x 8 291, 32 x 4 755; causal with
+// Query tiles as in the forward pass, but of 256 for heads of 128 with a bias, whose sums leave room for one workgroup a compute unit (2048 rows, 32
+// heads, us, tiles of 16 x 8 / 32 x 8 rows: 166 / 130).  Key tiles of heads of 128 have 16 keys a wavefront, as two
+// sums and two operands of 32 do not fit its registers (4096 rows, 16 heads, us: 16 x 4 296, 16 x 8 291, 32 x 4 755, or 377 with one wavefront a SIMD; causal with
 // grouped heads, 10374 rows: 745, 867, 2905).
-// The bias gradient's sums by distance, one set a wavefront, may leave no room for that many of them (borders beyond 1000 and heads of 128; fp32 beyond 460):
+// The bias gradient's sums by distance, one set a wavefront, may leave no room for that many of them (heads of 128: borders beyond some 700; fp32 460):
 // then fewer.
 template <typename T, int DP, int NB, int NW>
 constexpr int dq_lds(int last) {
@@ -208,8 +208,8 @@ BackwardPlan backward_plan(dchag_dtype dt, const AttendArgs& a) {
   p.q = tile_shape(dt, a.d, a.rows_q, a.sequences, a.heads, a.causal);
   p.k = tile_shape(dt, a.d, a.rows_k, a.sequences, a.kv_heads, true);
   if (a.d > 64) {
-    if (a.bias && p.q.nb == 2) p.q = {1, 8, 1};
-    if (p.q.nw == 8 && a.bias && dq_lds<bf16, 128, 1, 8>(a.last) > kLdsLimit) p.q = {1, 4, 2};
+    if (a.bias && p.q.nb == 2) p.q = {2, 8, 1};
+    if (p.q.nb == 2 && a.bias && dq_lds<bf16, 128, 2, 8>(a.last) > kLdsLimit) p.q = {1, 4, 2};
     if (dt == DCHAG_F32 && a.bias && dq_lds<float, 128, 1, 4>(a.last) > kLdsLimit) p.q = {1, 2, 1};
     if (p.k.nb == 2) p.k = {1, 4, 1};
   }
@@ -282,7 +282,7 @@ int backward_bias(const AttendArgs& a, const BackwardPlan& p, const BackwardPtrs
     }
   if (p.q.split == 2) rc = queries(Const<1>{}, Const<4>{}, Const<2>{});
   else if constexpr (sizeof(T) == 4) rc = queries(Const<1>{}, Const<4>{}, Const<1>{});
-  else if constexpr (DP == 128 && BIAS) rc = queries(Const<1>{}, Const<8>{}, Const<1>{});
+  else if constexpr (DP == 128 && BIAS) rc = queries(Const<2>{}, Const<8>{}, Const<1>{});
   else if constexpr (DP == 32) rc = queries(Const<2>{}, Const<4>{}, Const<1>{});
   else rc = p.q.nw == 8 ? queries(Const<2>{}, Const<8>{}, Const<1>{}) : queries(Const<2>{}, Const<4>{}, Const<1>{});
   return rc ? rc : rest_of_backward<T, DP, BIAS>(a, p, t, ws, st);
