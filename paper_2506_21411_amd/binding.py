@@ -548,7 +548,8 @@ def dchag_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: to
                  workspace: Optional[torch.Tensor] = None, stream=None):
     """(out [rows_q, heads, d], lse [heads, rows_q] float32) of attention over packed sequences: q [rows_q, heads, d], k and v
     [rows_k, kv_heads, d], int32 starts [sequences + 1] on the device.  Rows of a tensor may have gaps between them (columns of a
-    joint projection).  Rows of no sequence are not written: give an `out` of your own if they are read later."""
+    joint projection).  Rows of no sequence are not written: give an `out` of your own if they are read later.  Gradients:
+    dchag_attend_backward, called with what this returned (autograd does not know the calls)."""
     device = _device(q)
     ld_out = 0
     if out is not None:

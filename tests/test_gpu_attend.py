@@ -100,6 +100,7 @@ CASES = [
     dict(heads=2, kv=1, d=64, ql=[130, 40, 90, 50], kl=[70, 0, 200, 50], causal=True),
     dict(heads=2, kv=1, d=64, ql=[130, 40, 90], kl=[70, 0, 200], borders=LOG),
     dict(heads=2, kv=2, d=32, ql=[80, 70, 40], kl=[100, 90, 64], used=[100, 7, 0], causal=True, borders=LOG),
+    dict(heads=2, kv=1, d=64, ql=[90, 130], kl=[200, 130], used=[150, 1]),
 ]
 
 
@@ -351,6 +352,17 @@ def test_gradients_against_differences():
         have = float((got[name].double().cpu() * way).sum())
         size = float((got[name].double().cpu().abs() * way.abs()).sum())
         assert abs(have - want) <= 1e-5 * size + 1e-6, (name, have, want)        # differences: h^2, and fp32 gradients
+
+
+def test_bias_without_its_gradient():
+    p = Problem("bf16", 2, 2, 64, [100, 300], borders=LOG, seed=25, tail=0)
+    q, k, v, qs, ks = p.q.cuda(), p.k.cuda(), p.v.cuda(), dev(p.qs), dev(p.ks)
+    out, lse = dchag.dchag_attend(q, k, v, qs, ks, **p.kw())
+    dq, dk, dv, db = dchag.dchag_attend_backward(q, k, v, out, lse, p.dout.cuda(), qs, ks, want_dbias=False, **p.kw())
+    assert db is None
+    want = p.want()
+    del want["dbias"]
+    p.check(got={"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}, want=want)
 
 
 def test_scale_of_ones_own():
