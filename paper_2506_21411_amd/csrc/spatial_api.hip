@@ -86,11 +86,12 @@ struct TileShape {
   int nb, nw, split;
   int rows() const { return 16 * nb * nw / split; }
 };
-// Where tiles of 128 rows would leave compute units without work: tiles of 32, two wavefronts to a row (64 rows gave every SIMD one wavefront:
-// training step, 4 x 256 rows, 16 heads of 64, kernels' us 44 / 36), and for sequences that they hold whole (2048 of 24 rows, us: 1193 / 915).  fp32, whose fragments fill the registers, has 16 rows a wavefront: tiles of
-// 64, or of 32 as above where 64 leave SIMDs with less than two wavefronts (2 x 512 rows, 8 heads of 64, us: 120 / 82).  bf16: tiles of 256 for
-// long sequences whose rows see every key (heads of more than 32: a tile of keys is a load for each of 512 threads); otherwise of 128, since a causal
-// tile's work grows with its rows and short sequences fill large tiles badly (eight of 77 to 2048 rows, us, 128 / 256: 55 / 74).
+// Tiles of 32, two wavefronts to a row, where tiles of 128 rows would leave compute units without work (64 rows gave every SIMD one wavefront: training
+// step, 4 x 256 rows, 16 heads of 64, kernels' us 44 / 36), and for sequences that they hold whole (2048 of 24 rows, us: 1193 / 915).
+// fp32, whose fragments fill the registers, has 16 rows a wavefront: tiles of 64, or of 32 as above where 64 leave SIMDs with less than two
+// wavefronts (2 x 512 rows, 8 heads of 64, us: 120 / 82).  bf16 otherwise: tiles of 256 for long sequences whose rows see every key (heads of more
+// than 32: a tile of keys is a load for each of 512 threads), else of 128, since a causal tile's work grows with its rows and short sequences
+// fill large tiles badly (eight of 77 to 2048 rows, us, 128 / 256: 55 / 74).
 // 16 heads, 8192 rows, TFLOP/s with tiles of 64 / 128 / 256: heads of 64 714 / 799 / 839, heads of 128 836 / 1107 / 1152; causal, 32 heads of 128
 // 832 / 1069 / 1046.
 TileShape tile_shape(dchag_dtype dt, int d, long rows, long sequences, long heads, bool causal) {
@@ -103,11 +104,11 @@ TileShape tile_shape(dchag_dtype dt, int d, long rows, long sequences, long head
 
 template <int N> using Const = std::integral_constant<int, N>;
 
-// How a forward call goes about its rows: few (k_attend_few) or tiles of 64 nb rows.
+// How a forward call goes about its rows: few (k_attend_few) or tiles of query rows.
 struct ForwardPlan {
   bool few;
   TileShape tile;
-  long items, stretches;      // row tiles at most; few: parts that they are dealt to, 0: not split
+  long items, stretches;      // row tiles at most; few: parts that their keys are dealt to, 0: not split
   size_t part, part_ml, plan, total;
 };
 ForwardPlan forward_plan(dchag_dtype dt, const AttendArgs& a) {
