@@ -1033,9 +1033,10 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
 #pragma unroll
       for (int j = 0; j < 8; ++j) dot = fmaf(to_f32(dof[nb][ks][j]), to_f32(of[j]), dot);
     }
-    delta[nb] = row_sum(dot);
-    const float e = lse[(size_t)hi.h * a.rows_q + row];
-    lse2[nb] = in && e != kNegInf ? e * kLog2e : __builtin_inff();          // a row that sees no key: P = 0
+    const float sum = row_sum(dot), e = lse[(size_t)hi.h * a.rows_q + row];
+    const bool sees = in && e != kNegInf;
+    delta[nb] = sees ? sum : 0.f;                                            // a row that sees no key: P = 0, and what its dout holds has no part
+    lse2[nb] = sees ? e * kLog2e : __builtin_inff();
 #pragma unroll
     for (int b = 0; b < DB; ++b) acc[b][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
