@@ -324,8 +324,9 @@ size_t dchag_workspace_bytes(dchag_dtype dt, int B, int C, int H, int W, int p, 
  *   q, out [rows_q][heads][head_dim]     k, v [rows_k][kv_heads][head_dim]     lse [heads][rows_q] float
  *
  * A row that sees no key (Lk = 0, or causal and i + Lk - Lq < 0) has out = 0, lse = -inf, and no gradient.  Rows of
- * q and out (of k and v) that belong to no sequence are neither read nor written.  What a pair that is not visible holds
- * does not matter, nor do key rows that do not count: not even where they are not finite.
+ * q and out (of k and v) that belong to no sequence are neither read nor written, and key rows of a sequence that do not count
+ * are taken as if they belonged to none.  What a pair that is not visible holds does not matter, nor do key rows that do not
+ * count: not even where they are not finite.
  *
  * The bias is learned per head and bucket of relative positions: bucket(r) = the number of borders <= |r|, plus
  * n_borders + 1 if r > 0 and the call is not causal.  So bias is [heads][buckets] with buckets = n_borders + 1 (causal) or
@@ -361,7 +362,9 @@ int dchag_attend(dchag_dtype dt, const dchag_attention *att, const void *q, cons
 /*
  * Backward pass: gradients of a loss with dL/d(out) = dout.  out and lse are those of the forward call.
  *   dq, dk, dv   shaped like q, k, v        dbias [heads][buckets] or NULL (not wanted)
- * Gradients are overwritten, not accumulated into; gradients of shared key heads are sums over their group.  No sum uses
+ * Gradients of the sequences' rows are overwritten, not accumulated into.  Rows of no sequence, and key rows that do not count (k_used),
+ * whose gradient is zero, are left as they were: dk and dv start from zeros where such rows are read later, as when they are columns
+ * of one tensor that goes into a weight gradient.  Gradients of shared key heads are sums over their group.  No sum uses
  * atomics: results are reproducible run to run.  workspace: dchag_attend_workspace_bytes(dt, att, 1) bytes.
  * Errors: as dchag_attend; DCHAG_ERR_SHAPE for dbias without a bias.
  */

@@ -582,15 +582,17 @@ def dchag_attend_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out
                           dbias: Optional[torch.Tensor] = None, want_dbias: bool = True,
                           workspace: Optional[torch.Tensor] = None, stream=None):
     """(dq, dk, dv, dbias or None) of <dout, dchag_attend(...)>; out and lse are those of the forward call with the same arguments.
-    Rows of no sequence are not written."""
+    Rows of no sequence are not written.  Key rows that do not count (k_used) have no gradient: they are zero in the dk and dv that the call
+    makes, and left as they were, as rows of no sequence are, in a dk or dv of your own (clear it first if they are read later)."""
     device = _device(q)
     dt, dtype, lib, where = _dt(q), q.dtype, load_library(), q.device
     if dq is None:
         dq = torch.empty(q.shape, dtype=dtype, device=where)
+    room = torch.empty if k_used is None else torch.zeros          # the gradient of a key row that does not count
     if dk is None:
-        dk = torch.empty(k.shape, dtype=dtype, device=where)
+        dk = room(k.shape, dtype=dtype, device=where)
     if dv is None:
-        dv = torch.empty(k.shape, dtype=dtype, device=where)
+        dv = room(k.shape, dtype=dtype, device=where)
     if dbias is None and bias is not None and want_dbias:
         dbias = torch.empty(bias.shape, dtype=dtype, device=where)
     if dbias is not None and (bias is None or dbias.shape != bias.shape or not dbias.is_contiguous()):
