@@ -1125,8 +1125,9 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) delta[nb] = both(row_sum(sum[nb]));
   }
-  // Bias gradient: rows' sums of dS, which delta's error alone makes differ from 0, and of P in the last bucket of each side; the error's share
-  // of the last buckets is taken out at the end (2048 rows, 32 heads of 128: dbias' error against 64 bits 0.0031 -> 0.0016).
+  // With a bias: rows' sums of dS, which delta's error alone makes differ from 0, and of P in the last bucket of each side.  At the end the error's share
+  // of the last buckets is taken out (2048 rows, 32 heads of 128: dbias' error against 64 bits 0.0031 -> 0.0016), and delta goes to k_attend_dkv
+  // without it, whether dbias is wanted or not: dk does not depend on that.  (The near buckets keep their share, and so does dq.)
   float rest[NB], far_p[NB][2];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) rest[nb] = far_p[nb][0] = far_p[nb][1] = 0.f;
@@ -1162,7 +1163,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
         for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
           for (int r = 0; r < 4; ++r) s[mb][nb][r] *= dp[mb][nb][r] - delta[nb];
-      if (BIAS && want_dbias) {
+      if (BIAS) {
         float all = 0.f;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -1175,7 +1176,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
         if (!NEAR || side) {
           if (side < 0) sum_left += all;
           else sum_right += all;
-        } else {
+        } else if (want_dbias) {
           asm volatile("" ::: "memory");                                     // lanes read what other lanes of the wavefront wrote: in program order
           BiasGrad<NB>::put(pairs, s, lane);
           asm volatile("" ::: "memory");
@@ -1213,7 +1214,7 @@ __global__ __launch_bounds__(NW * 64, sizeof(T) == 2 ? 2 : 1) void k_attend_dq(A
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int i = iw + nb * 16 + l16;
-    if (BIAS && want_dbias) {
+    if (BIAS) {
       const float off_by = both(row_sum(rest[nb]));
       sum_left -= off_by * far_p[nb][0];
       sum_right -= off_by * far_p[nb][1];
