@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import inspect
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -498,8 +499,13 @@ def _raw_stream(device: int) -> int:
 
 def _on_stream(call):
     """Makes a call on the stream it is given, if it is given one: what the call allocates then is that stream's, too."""
+    at = list(inspect.signature(call).parameters).index("stream")  # past every argument that has a place, if it is a keyword
+
     @functools.wraps(call)
-    def on_stream(*args, stream=None, **kw):
+    def on_stream(*args, **kw):
+        if len(args) == at + 1 and "stream" not in kw:
+            args, kw["stream"] = args[:at], args[at]
+        stream = kw.get("stream")
         if stream is None:
             return call(*args, **kw)
         with torch.cuda.stream(stream):
