@@ -481,6 +481,13 @@ def _addr(t: torch.Tensor, dtype: torch.dtype, device: int, name: str) -> int:
     return t.data_ptr()
 
 
+def _bytes(workspace: torch.Tensor, device: int):
+    """Address and size of a workspace; like every tensor of a call it has to be on the current device, and in one piece."""
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("the workspace must be a contiguous tensor on the current device")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 def _vector(t: torch.Tensor, n: int, name: str) -> None:
     if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous vector of {n}")
@@ -574,8 +581,7 @@ def dchag_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: to
     if workspace is None:
         workspace = _workspace(lib.dchag_attend_workspace_bytes(dt, a, 0), where)
     _check(lib.dchag_attend(dt, a, _addr(q, dtype, device, "q"), _addr(k, dtype, device, "k"), _addr(v, dtype, device, "v"),
-                            _addr(out, dtype, device, "out"), _addr(lse, torch.float32, device, "lse"), workspace.data_ptr(),
-                            workspace.numel(), _raw_stream(device)))
+                            _addr(out, dtype, device, "out"), _addr(lse, torch.float32, device, "lse"), *_bytes(workspace, device), _raw_stream(device)))
     return out, lse
 
 
@@ -615,7 +621,7 @@ def dchag_attend_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out
         dt, a, _addr(q, dtype, device, "q"), _addr(k, dtype, device, "k"), _addr(v, dtype, device, "v"), _addr(out, dtype, device, "out"),
         _addr(lse, torch.float32, device, "lse"), _addr(dout, dtype, device, "dout"), _addr(dq, dtype, device, "dq"),
         _addr(dk, dtype, device, "dk"), _addr(dv, dtype, device, "dv"), None if dbias is None else _addr(dbias, dtype, device, "dbias"),
-        workspace.data_ptr(), workspace.numel(), _raw_stream(device)))
+        *_bytes(workspace, device), _raw_stream(device)))
     return dq, dk, dv, dbias
 
 
@@ -680,7 +686,7 @@ def dchag_weight_grad8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tens
         workspace = _workspace(lib.dchag_weight_grad8_workspace_bytes(dt, rows, d_out, d_in), dy.device)
     _check(lib.dchag_weight_grad8(dt, rows, d_out, d_in, ld, _addr(dy, dtype, device, "dy"), _addr(codes, torch.uint8, device, "codes"),
                                   _addr(scales, torch.uint8, device, "scales"), _addr(dW, dtype, device, "dW"),
-                                  None if db is None else _addr(db, dtype, device, "db"), workspace.data_ptr(), workspace.numel(), _raw_stream(device)))
+                                  None if db is None else _addr(db, dtype, device, "db"), *_bytes(workspace, device), _raw_stream(device)))
     return dW, db
 
 
