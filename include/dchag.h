@@ -334,10 +334,10 @@ size_t dchag_workspace_bytes(dchag_dtype dt, int B, int C, int H, int W, int p, 
  * values have to be finite).
  */
 typedef struct {
-  int32_t heads, kv_heads;          /* kv_heads divides heads                                            */
+  int32_t heads, kv_heads;          /* kv_heads divides heads; at most 4096 heads                        */
   int32_t head_dim;                 /* 8, 16, ..., 128                                                   */
   int32_t causal;                   /* 0 or 1                                                            */
-  int32_t sequences, rows_q, rows_k;/* >= 0                                                              */
+  int32_t sequences, rows_q, rows_k;/* 0 .. 2^30                                                         */
   float scale;                      /* > 0, or 0 for 1 / sqrt(head_dim)                                  */
   int64_t ld_q, ld_k, ld_v, ld_out; /* elements from one row to the next: a multiple of 8, at least the  */
   int64_t ld_dout, ld_dq, ld_dk, ld_dv; /* heads' columns, at most 2^23; 0 for rows without a gap.  The heads of a row

@@ -14,12 +14,17 @@ using namespace dchag;
 namespace {
 
 // ---- attention ------------------------------------------------------------------------------------------------------------
+// Rows and sequences are counted in 32 bits in the kernels, and so are a row's end plus a tile, a part of the keys plus another, and a key head's
+// pairs of (query, head of the group) where rows are few.  A part holds up to 2^30 keys: a sequence of more would be two parts where the workspace has
+// no room for parts (part_keys).
+constexpr int kMostRows = 1 << 30;
 int check_attention(dchag_dtype dt, const dchag_attention* a) {
   if (dt != DCHAG_F32 && dt != DCHAG_BF16) return DCHAG_ERR_DTYPE;
   if (!a || !a->q_starts || !a->k_starts) return DCHAG_ERR_NULL;
   if (a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->heads > 4096) return DCHAG_ERR_SHAPE;
   if (a->head_dim < 8 || a->head_dim > 128 || a->head_dim % 8) return DCHAG_ERR_SHAPE;
   if (a->sequences < 0 || a->rows_q < 0 || a->rows_k < 0 || (a->causal != 0 && a->causal != 1)) return DCHAG_ERR_SHAPE;
+  if (a->sequences > kMostRows || a->rows_q > kMostRows || a->rows_k > kMostRows) return DCHAG_ERR_SHAPE;
   if (!(a->scale >= 0.f) || !(a->scale < INFINITY)) return DCHAG_ERR_SHAPE;
   const int64_t lds[8] = {a->ld_q, a->ld_k, a->ld_v, a->ld_out, a->ld_dout, a->ld_dq, a->ld_dk, a->ld_dv};
   const int heads_of[8] = {a->heads, a->kv_heads, a->kv_heads, a->heads, a->heads, a->heads, a->kv_heads, a->kv_heads};
@@ -119,7 +124,7 @@ ForwardPlan forward_plan(dchag_dtype dt, const AttendArgs& a) {
   // Few rows: on average at most as many as a row tile has, of grouped heads two tiles' (the other kernel reads the keys once a head), and
   // many keys or hardly any rows.  us, few / tiles of 32 rows: 64 sequences, 2000 keys, 16 heads, 10 rows 104 / 105, 20 rows 133 / 106; 32 heads on 8,
   // 5 rows 56 / 73; 2048 sequences of 10 rows and keys 200 / 132.
-  p.few = rows <= (group > 1 ? 2L : 1L) * kFewRows * seqs && (a.rows_k >= 128 * seqs || rows <= 4 * seqs);
+  p.few = rows <= (group > 1 ? 2L : 1L) * kFewRows * seqs && (a.rows_k >= 128 * seqs || rows <= 4 * seqs) && rows <= kMostRows;
   if (p.few) {
     p.items = rows / kFewRows + std::min<long>(a.sequences, rows);
     const long fill = 4L * compute_units() / a.kv_heads;                     // twice the workgroups that the chip holds at once
