@@ -354,7 +354,8 @@ typedef struct {
  * Forward pass.  out may not overlap the inputs.  workspace: dchag_attend_workspace_bytes(dt, att, 0) bytes, 256-byte aligned.
  * Results do not depend on what other sequences a call holds, nor on how often it runs, up to the choice of kernel, which
  * goes by rows_q, rows_k, sequences and the head counts.
- * Errors: NULL att, starts, or a tensor that has rows; heads % kv_heads; head_dim; row strides; borders (DCHAG_ERR_SHAPE).
+ * Errors: NULL att, starts, or a tensor that has rows; heads % kv_heads; head_dim; row strides; borders; more row tiles times heads than a launch
+ * has room for (2^32 threads: a row tile of 32 to 256 rows, or a sequence's part of one, is 256 or 512) (DCHAG_ERR_SHAPE).
  */
 int dchag_attend(dchag_dtype dt, const dchag_attention *att, const void *q, const void *k, const void *v,
                  void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
@@ -385,7 +386,8 @@ size_t dchag_attend_workspace_bytes(dchag_dtype dt, const dchag_attention *att, 
  * so that scaling is exact, nothing saturates, and the one rounding (to nearest, ties to even) is off by at most 2^-4 of a value, or
  * 2^-10 * 2^(byte - 127) where that is more.  (A value beyond 1.875 * 2^127 becomes that.)  A value that is not finite is kept as NaN.
  *   x [rows][D] with ld elements from row to row (0: D)      codes [rows][D]      scales [rows][(D + 31) / 32]
- * Errors: NULL pointers; D % 8 != 0, D < 8, D > 2^20; ld < D, ld % 8 != 0 or ld > 2^23; rows < 0.
+ * Errors: NULL pointers; D % 8 != 0, D < 8, D > 2^20; ld < D, ld % 8 != 0 or ld > 2^23; rows < 0; more blocks than the threads of a
+ * launch can take (a little under 2^32: blocks of 32 to pack, 2^30 to unpack; take the rows in parts).
  */
 int dchag_pack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void *x, void *codes, void *scales, void *stream);
 int dchag_unpack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void *codes, const void *scales, void *x, void *stream);

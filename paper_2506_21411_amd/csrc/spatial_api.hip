@@ -13,6 +13,10 @@ using namespace dchag;
 
 namespace {
 
+// The threads of a launch are counted in 32 bits.
+constexpr long kMostThreads = 0xffffffffL;
+bool too_large(long workgroups, int threads) { return workgroups > kMostThreads / threads; }
+
 // ---- attention ------------------------------------------------------------------------------------------------------------
 // Rows and sequences are counted in 32 bits in the kernels, and so are a row's end plus a tile, a part of the keys plus another, and a key head's
 // pairs of (query, head of the group) where rows are few.  A part holds up to 2^30 keys: a sequence of more would be two parts where the workspace has
@@ -323,10 +327,10 @@ GradPlan grad_plan(dchag_dtype dt, long rows, int d_out, int d_in) {
   p.total = p.splits > 1 ? align_up(((size_t)p.splits * d_out * d_in + (size_t)p.splits * d_out) * 4) : 256;
   return p;
 }
-int check_rows8(dchag_dtype dt, int64_t rows, int D, int64_t ld) {
+int check_rows8(dchag_dtype dt, int64_t rows, int D, int64_t ld, int turns) {
   if (dt != DCHAG_F32 && dt != DCHAG_BF16) return DCHAG_ERR_DTYPE;
   if (rows < 0 || D < 8 || D % 8 || D > (1 << 20) || (ld != 0 && (ld < D || ld % 8 || ld > (1 << 23)))) return DCHAG_ERR_SHAPE;
-  if (rows > (int64_t)0x7fffffff * 64 / ((D + 31) / 32)) return DCHAG_ERR_SHAPE;   // workgroups of 64 blocks
+  if (rows > kMostThreads / 1024 * 256 * turns / ((D + 31) / 32)) return DCHAG_ERR_SHAPE;   // four threads a block of 32, of whole workgroups
   return DCHAG_OK;
 }
 Rows8 rows8(int64_t rows, int D, int64_t ld) {
@@ -385,7 +389,7 @@ int dchag_attend(dchag_dtype dt, const dchag_attention* att, const void* q, cons
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(lse)) return DCHAG_ERR_ALIGN;
   const ForwardPlan p = forward_plan(dt, a);
   if (bad_workspace(workspace, workspace_bytes, p.total)) return DCHAG_ERR_WORKSPACE;
-  if ((p.few ? std::max(p.items, p.stretches) * a.kv_heads : p.items * a.heads) > 0x7fffffffL) return DCHAG_ERR_SHAPE;
+  if (p.few ? too_large(std::max(p.items, p.stretches) * a.kv_heads, 256) : too_large(p.items * a.heads, p.tile.nw * 64)) return DCHAG_ERR_SHAPE;
   if (p.items == 0) return DCHAG_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
@@ -417,7 +421,7 @@ int dchag_attend_backward(dchag_dtype dt, const dchag_attention* att, const void
     return DCHAG_ERR_ALIGN;
   const BackwardPlan p = backward_plan(dt, a);
   if (bad_workspace(workspace, workspace_bytes, p.total)) return DCHAG_ERR_WORKSPACE;
-  if (p.items_q * a.heads > 0x7fffffffL || p.items_k * a.kv_heads > 0x7fffffffL) return DCHAG_ERR_SHAPE;
+  if (too_large(p.items_q * a.heads, p.q.nw * 64) || too_large(p.items_k * a.kv_heads, 256)) return DCHAG_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   BackwardPtrs t{q, k, v, out, dout, lse, dq, dk, dv, dbias, nullptr, nullptr};
@@ -436,7 +440,7 @@ int dchag_attend_backward(dchag_dtype dt, const dchag_attention* att, const void
 }
 
 int dchag_pack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void* x, void* codes, void* scales, void* stream) {
-  int rc = check_rows8(dt, rows, D, ld);
+  int rc = check_rows8(dt, rows, D, ld, kTurns);
   if (rc) return rc;
   if (rows == 0) return DCHAG_OK;
   if (!x || !codes || !scales) return DCHAG_ERR_NULL;
@@ -452,7 +456,7 @@ int dchag_pack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void* x, 
 }
 
 int dchag_unpack8(dchag_dtype dt, int64_t rows, int D, int64_t ld, const void* codes, const void* scales, void* x, void* stream) {
-  int rc = check_rows8(dt, rows, D, ld);
+  int rc = check_rows8(dt, rows, D, ld, 1);
   if (rc) return rc;
   if (rows == 0) return DCHAG_OK;
   if (!x || !codes || !scales) return DCHAG_ERR_NULL;
