@@ -343,7 +343,8 @@ typedef struct {
   int64_t ld_dout, ld_dq, ld_dk, ld_dv; /* heads' columns, at most 2^23; 0 for rows without a gap.  The heads of a row
                                        lie one behind the other (q, k and v may be columns of one tensor) */
   const int32_t *q_starts, *k_starts;/* DEVICE, [sequences + 1], not decreasing.  Values outside 0 .. rows are taken as the
-                                       nearest inside: a call never leaves its tensors                   */
+                                       nearest inside, and a start behind the next one as an empty sequence: a call never
+                                       leaves its tensors (but rows of several sequences have undefined results) */
   const int32_t *k_used;            /* DEVICE, [sequences], or NULL: all key rows count                  */
   const void *bias;                 /* [heads][buckets], type dt, or NULL: no bias                       */
   const int32_t *borders;           /* HOST, [n_borders], with a bias: increasing, from >= 1 to <= 1024  */

@@ -233,7 +233,7 @@ __device__ __forceinline__ bool find_span(const AttendArgs& a, int idx, Count co
     read_span(a, s, sp.q0, sp.nq, sp.k0, sp.nk);
     sp.tiles = count(sp.nq, sp.nk);
     sp.tile = idx - a.firsts[s];
-    return true;
+    return sp.tile >= 0 && sp.tile < sp.tiles;                               // false only where overlapping sequences have more items than 32 bits count
   }
   for (int s0 = 0; s0 < a.sequences; s0 += 64) {
     int q0 = 0, nq = 0, k0 = 0, nk = 0, n = 0;
@@ -590,6 +590,11 @@ __device__ __forceinline__ int wave_total(int v) {
   for (int w = 1; w < 64; w *= 2) v += __shfl_xor(v, w);
   return __builtin_amdgcn_readfirstlane(v);
 }
+__device__ __forceinline__ long wave_total(long v) {
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) v += __shfl_xor(v, w);
+  return (long)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
 // The keys of a part, of `keys` in all row tiles together.
 __device__ __forceinline__ int part_keys(const AttendArgs& a, int stretches, int tiles, long keys) {
   const int spare = stretches - tiles;
@@ -608,10 +613,11 @@ __device__ __forceinline__ bool find_stretch(const AttendArgs& a, int stretches,
     st.sp.tiles = (st.sp.nq * group + kFewRows - 1) / kFewRows;
     st.parts = max(1, (st.sp.nk + st.keys - 1) / st.keys);
     const int inside = at - of[s];
+    if (inside < 0) return false;                                            // see find_span
     st.sp.tile = by_tile ? inside : inside / st.parts;
     st.part = by_tile ? 0 : inside % st.parts;
     st.first = a.firsts[s] + st.sp.tile * st.parts;
-    return true;
+    return st.sp.tile < st.sp.tiles;
   }
   const int lane = threadIdx.x & 63, group = a.heads / a.kv_heads;
   long keys = 0;
@@ -622,8 +628,7 @@ __device__ __forceinline__ bool find_stretch(const AttendArgs& a, int stretches,
     if (s0 + lane < a.sequences) read_span(a, s0 + lane, q0, nq, k0, nk);
     const int n = (nq * group + kFewRows - 1) / kFewRows;
     tiles += wave_total(n);
-    keys += (long)wave_total(n * (nk >> 10)) << 10;                          // in 1024s and the rest: no 32-bit overflow
-    keys += wave_total(n * (nk & 1023));
+    keys += wave_total((long)n * nk);                                        // overlapping sequences: more than 32 bits even in 1024s
   }
   st.keys = part_keys(a, stretches, tiles, keys);
   int first = 0;
@@ -911,6 +916,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int stretches
   const int group = a.heads / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
   Stretch where;
   if (!find_stretch(a, stretches, blockIdx.x / a.kv_heads, true, where) || where.parts == 1) return;
+  if (where.first < 0 || where.parts > stretches - where.first) return;      // as in find_span
   const Span& sp = where.sp;
   const size_t pitch = (size_t)a.kv_heads * kFewRows;                        // rows of partial results from one part to the next
   for (int e = threadIdx.x; e < kFewRows * DP / 4; e += 256) {
