@@ -353,8 +353,10 @@ typedef struct {
 
 /*
  * Forward pass.  out may not overlap the inputs.  workspace: dchag_attend_workspace_bytes(dt, att, 0) bytes, 256-byte aligned.
- * Results do not depend on what other sequences a call holds, nor on how often it runs, up to the choice of kernel, which
- * goes by rows_q, rows_k, sequences and the head counts.
+ * The same call gives the same bits every time.  A sequence's results do not depend on what other sequences a call holds, but for the
+ * order of their sums: the choice of kernel goes by rows_q, rows_k, sequences and the head counts, and where few rows meet many keys, the
+ * length of the parts that keys are cut into goes by the counted keys of all sequences, so that one cache's growth may change the others'
+ * last bits.
  * Errors: NULL att, starts, or a tensor that has rows; heads % kv_heads; head_dim; row strides; borders; more row tiles times heads than a launch
  * has room for (2^32 threads: a row tile of 32 to 256 rows, or a sequence's part of one, is 256 or 512) (DCHAG_ERR_SHAPE).
  */
@@ -362,8 +364,10 @@ int dchag_attend(dchag_dtype dt, const dchag_attention *att, const void *q, cons
                  void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * Backward pass: gradients of a loss with dL/d(out) = dout.  out and lse are those of the forward call.
- *   dq, dk, dv   shaped like q, k, v        dbias [heads][buckets] or NULL (not wanted)
+ * Backward pass: gradients of a loss with dL/d(out) = dout.  out and lse are those of the forward call with the same arguments: the
+ * kernels use that the weights of a row, exp(s_ij - lse_i), add up to 1 over the call's keys.  (An out and lse joined from calls over parts of
+ * the keys do not go with one part; gradients are formed by a call over all of them.)
+ *   dq, dk, dv   shaped like q, k, v, not overlapping the inputs        dbias [heads][buckets] or NULL (not wanted)
  * Gradients of the sequences' rows are overwritten, not accumulated into.  Rows of no sequence, and key rows that do not count (k_used),
  * whose gradient is zero, are left as they were: dk and dv start from zeros where such rows are read later, as when they are columns
  * of one tensor that goes into a weight gradient.  Gradients of shared key heads are sums over their group.  No sum uses

@@ -131,7 +131,8 @@ __global__ __launch_bounds__(256) void k_unpack8(Rows8 r, const unsigned char* _
   store8(x + at, v);
 }
 
-// dW[o][i] = sum over rows of dy[row][o] x[row][i], db[o] = sum of dy[row][o], x held in 8 bits.  MFMA-bound for long inputs.
+// dW[o][i] = sum over rows of dy[row][o] x[row][i], db[o] = sum of dy[row][o], x held in 8 bits.  For long inputs no unit is full: matrix instructions
+// take 52 % of the busy cycles, LDS 27 % (1536 x 1024 over 32768 rows), and the loop without its loads 95 of 107 us.
 // Workgroup: OS x IS of dW over one stretch of the rows, its wavefronts NO x NI parts of 16 WO x 16 WI; slices of 64 rows of
 // both operands lie in LDS as they lie in memory (both have the sum's index as their row) and are read transposed.  dy comes by
 // direct-to-LDS loads; of x a thread takes half a block of 32 codes or a whole one, which it turns into numbers of T once for all that read them: every
